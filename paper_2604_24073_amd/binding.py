@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
-from typing import Dict, Optional
+from typing import Dict, NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -42,6 +42,17 @@ class fs_step_args(ctypes.Structure):
         ("reduced", c_vp), ("emb_t1", c_vp),
         ("co_flag_t1", c_vp),
         ("sorted_ids_t1", c_vp),
+    ]
+
+
+class fs_block_args(ctypes.Structure):
+    _fields_ = [
+        ("n", c_i64), ("dim", c_i32), ("rows_dt", c_i32), ("dt", c_i32), ("eps", c_f),
+        ("x", c_vp), ("a", c_vp), ("g", c_vp), ("a_stride", c_i64), ("g_stride", c_i64),
+        ("w_post", c_vp), ("scale", c_vp), ("w_pre", c_vp), ("y", c_vp), ("h", c_vp),
+        ("a_codes", c_vp), ("g_codes", c_vp), ("y_codes", c_vp), ("a_exps", c_vp), ("g_exps", c_vp), ("y_exps", c_vp),
+        ("dy", c_vp), ("dh", c_vp), ("dx", c_vp), ("da", c_vp), ("dg", c_vp), ("da_stride", c_i64), ("dg_stride", c_i64),
+        ("dw_post", c_vp), ("dscale", c_vp), ("dw_pre", c_vp), ("work", c_vp), ("work_bytes", ctypes.c_size_t),
     ]
 
 
@@ -121,6 +132,11 @@ def load_library() -> ctypes.CDLL:
         "fs_ctx_set_kernel_timing": (ctypes.c_int, [c_vp, ctypes.c_int, ctypes.c_int]),
         "fs_ctx_get_kernel_timing": (ctypes.c_int, [c_vp, ctypes.c_int, ctypes.POINTER(c_f), ctypes.c_int,
                                                     ctypes.POINTER(ctypes.c_int)]),
+        "fs_rows_pack8": (ctypes.c_int, [c_vp, c_vp, c_i64, ctypes.c_int, c_i64, c_i32, c_vp, c_vp, S]),
+        "fs_rows_unpack8": (ctypes.c_int, [c_vp, c_vp, c_vp, c_i64, c_i32, c_vp, c_i64, ctypes.c_int, S]),
+        "fs_block_norm": (ctypes.c_int, [c_vp, ctypes.POINTER(fs_block_args), S]),
+        "fs_block_norm_backward": (ctypes.c_int, [c_vp, ctypes.POINTER(fs_block_args), S]),
+        "fs_block_norm_work_bytes": (ctypes.c_size_t, [c_i64, c_i32]),
         "fs_init_table_hash": (ctypes.c_int, [c_vp, c_vp, c_i64, c_i32, ctypes.c_int, S]),
         "fs_stream_copy": (ctypes.c_int, [c_vp, c_vp, c_vp, c_i64, S]),
         "fs_stream_row_read": (ctypes.c_int, [c_vp, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, S]),
@@ -659,3 +675,201 @@ def make_step_args(table: torch.Tensor, state: torch.Tensor, lr: float, eps: flo
     a.co_flag_t1 = _ptr(split.get("co_flag_t1"))
     a.reduced = _ptr(reduced)
     return a
+
+
+# ---- the history encoder (include/freescale_encoder.h) ----------------------------------------------------------------
+FS_ROWS8_GROUP = 32
+FS_MAX_BLOCK_DIM = 1024
+
+
+class Rows8(NamedTuple):
+    """Rows in 8 bits: codes int8 [n, dim], exps uint8 [n, dim / FS_ROWS8_GROUP]."""
+    codes: torch.Tensor
+    exps: torch.Tensor
+
+
+def _ctx_stream(ctx: Context, stream):
+    """The stream of a call: the current one of the context's GPU, which need not be the current GPU."""
+    if stream is None and _current_raw_stream is not None:
+        return _current_raw_stream(ctx.device) or None
+    return _stream(torch.cuda.current_stream(ctx.device) if stream is None else stream)
+
+
+def _scratch(ctx: Context, nbytes: int, handle) -> torch.Tensor:
+    """Scratch memory that is given back when the call has been enqueued: on the stream of the call, so that what torch makes
+    of it next waits for the call."""
+    current = torch.cuda.current_stream(ctx.device)
+    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=f"cuda:{ctx.device}")
+    if handle != (current.cuda_stream or None):
+        work.record_stream(torch.cuda.ExternalStream(handle or 0, device=ctx.device))
+    return work
+
+
+def _on(ctx: Context, what: str, *tensors) -> None:
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != ctx.device):
+            raise ValueError(f"{what}: tensor on {t.device}, the context is on cuda:{ctx.device}")
+
+
+def _rows2(what: str, t: torch.Tensor, n: int, dim: int, dtype=None, packed: bool = True) -> torch.Tensor:
+    """[n, dim] with its columns next to each other, and its rows too where `packed`."""
+    if t.dim() != 2 or tuple(t.shape) != (n, dim):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(n, dim)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what}: {t.dtype}, expected {dtype}")
+    if (dim > 1 and t.stride(1) != 1) or (packed and n > 1 and t.stride(0) != dim):
+        raise ValueError(f"{what}: strides {t.stride()}" + (", a contiguous tensor is needed" if packed else ""))
+    return t
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _weights(what: str, t: torch.Tensor, dim: int) -> torch.Tensor:
+    if t.dtype != torch.float32 or t.numel() != dim or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous fp32 tensor of {dim} values is needed")
+    return t
+
+
+def _rows8(what: str, t: Rows8, n: int, dim: int) -> Rows8:
+    if (t.codes.dtype != torch.int8 or t.exps.dtype != torch.uint8 or t.codes.numel() != n * dim
+            or t.exps.numel() * FS_ROWS8_GROUP != n * dim or not t.codes.is_contiguous() or not t.exps.is_contiguous()):
+        raise ValueError(f"{what}: not the {n} x {dim} rows in 8 bits that are expected here")
+    return t
+
+
+def _alloc_rows8(n: int, dim: int, device) -> Rows8:
+    return Rows8(torch.empty((n, dim), dtype=torch.int8, device=device),
+                 torch.empty((n, dim // FS_ROWS8_GROUP), dtype=torch.uint8, device=device))
+
+
+def fs_rows_pack8(ctx: Context, rows: torch.Tensor, out: Optional[Rows8] = None, stream=None) -> Rows8:
+    n, dim = rows.shape
+    _rows2("rows", rows, n, dim, packed=False)
+    out = _alloc_rows8(n, dim, rows.device) if out is None else _rows8("out", out, n, dim)
+    _on(ctx, "fs_rows_pack8", rows, *out)
+    rc = ctx.lib.fs_rows_pack8(ctx.handle, _ptr(rows), _row_stride(rows), table_dtype_code(rows), n, dim, _ptr(out.codes),
+                               _ptr(out.exps), _ctx_stream(ctx, stream))
+    ctx.check(rc, "fs_rows_pack8")
+    return out
+
+
+def fs_rows_unpack8(ctx: Context, packed: Rows8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    n, dim = packed.codes.shape
+    _rows8("packed", packed, n, dim)
+    if out is None:
+        out = torch.empty((n, dim), dtype=dtype, device=packed.codes.device)
+    _rows2("out", out, n, dim, packed=False)
+    _on(ctx, "fs_rows_unpack8", out, *packed)
+    rc = ctx.lib.fs_rows_unpack8(ctx.handle, _ptr(packed.codes), _ptr(packed.exps), n, dim, _ptr(out), _row_stride(out),
+                                 table_dtype_code(out), _ctx_stream(ctx, stream))
+    ctx.check(rc, "fs_rows_unpack8")
+    return out
+
+
+def fs_block_norm(ctx: Context, x: torch.Tensor, a: Optional[torch.Tensor] = None, g: Optional[torch.Tensor] = None,
+                  w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                  w_pre: Optional[torch.Tensor] = None, eps: float = 1e-6, pack: Sequence[str] = (),
+                  dtype: Optional[torch.dtype] = None, out: Optional[Dict] = None, stream=None) -> Dict:
+    """y (where a is given) and h (where w_pre is given); pack: which of "a", "g", "y" are wanted in 8 bits too, as a8, g8,
+    y8.  dtype: that of h where there is no a.  `out`: the caller's tensors under the same names."""
+    n, dim = x.shape
+    rec = fs_block_args(n=n, dim=dim, rows_dt=table_dtype_code(x), eps=eps, x=_ptr(_rows2("x", x, n, dim)))
+    given, res = dict(out or {}), {}
+    act = a.dtype if a is not None else dtype or x.dtype
+    wanted = [("y", x.dtype)] if a is not None else []
+    if w_pre is not None:
+        wanted.append(("h", act))
+        rec.w_pre = _ptr(_weights("w_pre", w_pre, dim))
+    for name, dt in wanted:
+        res[name] = _rows2(name, given[name], n, dim, dt) if name in given else torch.empty((n, dim), dtype=dt, device=x.device)
+        setattr(rec, name, _ptr(res[name]))
+    if a is not None:
+        _rows2("a", a, n, dim, packed=False), _rows2("g", g, n, dim, act, packed=False)
+        rec.a, rec.g, rec.a_stride, rec.g_stride = _ptr(a), _ptr(g), _row_stride(a), _row_stride(g)
+        rec.w_post, rec.scale = _ptr(_weights("w_post", w_post, dim)), _ptr(_weights("scale", scale, dim))
+    rec.dt = table_dtype_code(a if a is not None else res["h"] if "h" in res else x)
+    for name in pack:
+        if name not in ("a", "g", "y") or (a is None and name != "y"):
+            raise ValueError(f"pack: no {name!r} to pack")
+        key = name + "8"
+        res[key] = _rows8(key, given[key], n, dim) if key in given else _alloc_rows8(n, dim, x.device)
+        setattr(rec, name + "_codes", _ptr(res[key].codes))
+        setattr(rec, name + "_exps", _ptr(res[key].exps))
+    _on(ctx, "fs_block_norm", x, a, g, w_post, scale, w_pre,
+        *(t for v in res.values() for t in (v if isinstance(v, Rows8) else (v,))))
+    ctx.check(ctx.lib.fs_block_norm(ctx.handle, ctypes.byref(rec), _ctx_stream(ctx, stream)), "fs_block_norm")
+    return res
+
+
+def fs_block_norm_backward(ctx: Context, dy: Optional[torch.Tensor], dh: Optional[torch.Tensor],
+                           a: Union[torch.Tensor, Rows8, None] = None, g: Union[torch.Tensor, Rows8, None] = None,
+                           y: Union[torch.Tensor, Rows8, None] = None, w_post: Optional[torch.Tensor] = None,
+                           scale: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                           dtype: Optional[torch.dtype] = None, rows_dtype: Optional[torch.dtype] = None,
+                           out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """dx, and da, dg, dw_post, dscale where a is given, dw_pre where dh is given.  a, g, y: as the forward pass had or left
+    them, or its a8, g8, y8.  dtype, rows_dtype: those of the block's rows and of the residual rows, where no tensor given
+    tells."""
+    some = next(t for t in (dy, dh, a, y) if t is not None)
+    shape = some.codes.shape if isinstance(some, Rows8) else some.shape
+    n, dim = shape
+    device = some.codes.device if isinstance(some, Rows8) else some.device
+    plain = lambda *ts: next((t.dtype for t in ts if isinstance(t, torch.Tensor)), None)  # noqa: E731
+    rows_dt = plain(dy, y) or rows_dtype or torch.float32
+    act = plain(dh, a, g) or dtype or rows_dt
+    codes = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
+    if rows_dt not in codes or act not in codes:
+        raise TypeError(f"{rows_dt}, {act}: fp32 or bf16 only")
+    rec = fs_block_args(n=n, dim=dim, rows_dt=codes[rows_dt], dt=codes[act], eps=eps)
+    given, res, used = dict(out or {}), {}, [dy, dh]
+
+    def output(name, shape, dt):
+        t = given[name] if name in given else torch.empty(shape, dtype=dt, device=device)
+        if len(shape) == 1:
+            _weights(name, t, shape[0])
+        else:
+            _rows2(name, t, n, dim, dt, packed=name == "dx")
+        res[name] = t
+        setattr(rec, name, _ptr(t))
+
+    def kept(name, t, dt, packed):
+        if isinstance(t, Rows8):
+            _rows8(name, t, n, dim)
+            setattr(rec, name + "_codes", _ptr(t.codes))
+            setattr(rec, name + "_exps", _ptr(t.exps))
+            used.extend(t)
+            return
+        _rows2(name, t, n, dim, dt, packed=packed)
+        setattr(rec, name, _ptr(t))
+        used.append(t)
+
+    output("dx", (n, dim), rows_dt)
+    if dy is not None:
+        rec.dy = _ptr(_rows2("dy", dy, n, dim, rows_dt))
+    if dh is not None:
+        rec.dh = _ptr(_rows2("dh", dh, n, dim, act))
+        rec.w_pre = _ptr(_weights("w_pre", w_pre, dim))
+        kept("y", y, rows_dt, True)
+        output("dw_pre", (dim,), torch.float32)
+    if a is not None:
+        kept("a", a, act, False)
+        kept("g", g, act, False)
+        rec.a_stride = _row_stride(a) if isinstance(a, torch.Tensor) else 0
+        rec.g_stride = _row_stride(g) if isinstance(g, torch.Tensor) else 0
+        rec.w_post, rec.scale = _ptr(_weights("w_post", w_post, dim)), _ptr(_weights("scale", scale, dim))
+        for name in ("da", "dg"):
+            output(name, (n, dim), act)
+        rec.da_stride, rec.dg_stride = _row_stride(res["da"]), _row_stride(res["dg"])
+        for name in ("dw_post", "dscale"):
+            output(name, (dim,), torch.float32)
+    _on(ctx, "fs_block_norm_backward", *used, w_post if a is not None else None, scale if a is not None else None,
+        w_pre if dh is not None else None, *res.values())
+    handle = _ctx_stream(ctx, stream)
+    nbytes = ctx.lib.fs_block_norm_work_bytes(n, dim)
+    work = _scratch(ctx, nbytes, handle)
+    rec.work, rec.work_bytes = _ptr(work), work.numel()
+    ctx.check(ctx.lib.fs_block_norm_backward(ctx.handle, ctypes.byref(rec), handle), "fs_block_norm_backward")
+    return res
