@@ -91,6 +91,76 @@ int fs_block_norm(fs_ctx *ctx, const fs_block_args *args, fs_stream stream);
 int fs_block_norm_backward(fs_ctx *ctx, const fs_block_args *args, fs_stream stream);
 size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
 
+/* ---- attention over a jagged batch -------------------------------------------------------------------- */
+
+#define FS_MAX_HEAD_DIM 128
+#define FS_MAX_BIAS_BUCKETS 1024
+#define FS_MAX_BIAS_DISTANCES 4096
+
+/* Attention of each user's query rows over the user's keys and values, with a learned bias for the bucket that the distance
+ * between the two lies in:
+ *     s_ij = scale q_i . k_j + bias[bucket(pos_i - pos_j), head]      o_i = sum over j of softmax(s_i)_j v_j
+ * User b has the query rows q_offsets[b] .. q_offsets[b+1] and the keys kv_offsets[b] .. kv_offsets[b+1], of which the first
+ * kv_lengths[b] are in use (kv_lengths == NULL: all; a cache that grows has rows to spare).  The query rows are the last ones
+ * of the history: with nk keys in use and nq query rows, row i stands at position nk - nq + i, key j at j.  For a batch
+ * that attends to itself q_offsets and kv_offsets are the same.
+ *   causal == 1: row i sees the keys up to its own position; == 0: all keys in use.  A row that sees no key (there are more
+ *         query rows than keys, or every bias it meets is -infinity) gives zeros, and no gradient.  What a row does not see
+ *         does not reach it, infinities and NaN included.
+ *   q [n_q, heads, head_dim], k and v [n_kv, kv_heads, head_dim] of dt, heads of a row next to each other, rows q_stride,
+ *         k_stride, v_stride elements apart; query heads h .. h + heads/kv_heads - 1 share a key head
+ *   bias  [num_buckets, heads] fp32 (NULL: none), bucket_of int32: the bucket of each distance, tabulated by the caller -
+ *         causal: [num_distances] for the distances 0, 1, ...; else [2 num_distances - 1] for -(num_distances - 1) ...
+ *         num_distances - 1.  Distances beyond the table are its last entry on that side.  A bucket out of range counts as
+ *         no bias and is reported as FS_ERANGE by fs_check_async.
+ *   out   [n_q, heads, head_dim] of dt, packed
+ *   lse   [heads, n_q] fp32 (OPTIONAL; the backward pass reads it): log of the sum of exp(s_i), -infinity for a row that sees
+ *         nothing
+ *   out_f32 [n_q, heads, head_dim] fp32 (OPTIONAL, bf16 only): out before its rounding.  The backward pass reads it where it
+ *         is given: without it, dbias carries the roundings of out.
+ *   max_q no user has more query rows than this (0: unknown).  With max_q * heads / kv_heads <= 16 the keys are cut up over
+ *         the chip, which is the form for single tokens; a user with more rows is then reported as FS_ERANGE and its rows of
+ *         out are left as they were.
+ *   work  fs_jagged_attention_work_bytes(args) bytes, 16-byte aligned, contents irrelevant (0 bytes and NULL but for the form
+ *         above)
+ * Scores, softmax and sums are in fp32; P and dS are rounded to dt where they go into a product.  head_dim
+ * a multiple of 4 (fp32) / 8 (bf16), at most FS_MAX_HEAD_DIM.  (rows / 64 + batch) * heads < 2^24, a user has fewer than 2^30 rows.  Boundaries that do not ascend
+ * from 0 to n_q (n_kv) and lengths that do not fit their room are reported as FS_ERANGE by fs_check_async; out of the user
+ * concerned is not written or is that of the keys there are. */
+typedef struct fs_attention_args {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    int64_t n_q, n_kv, batch;
+    const int64_t *q_offsets, *kv_offsets, *kv_lengths;
+    int32_t heads, kv_heads, head_dim;
+    int32_t dt;                      /* fs_dtype */
+    int32_t causal, max_q;
+    float scale;
+    int32_t num_buckets, num_distances;
+    const float *bias;
+    const int32_t *bucket_of;
+    void *out;
+    float *out_f32, *lse;
+    /* backward only */
+    const void *dout;
+    void *dq, *dk, *dv;
+    int64_t dq_stride, dk_stride, dv_stride;
+    float *dbias;
+    void *work;
+    size_t work_bytes;
+} fs_attention_args;
+
+int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream stream);
+size_t fs_jagged_attention_work_bytes(const fs_attention_args *args);
+
+/* Its gradients, from dout [n_q, heads, head_dim] of dt (packed) and out, lse and out_f32 as the forward pass left them:
+ *     dq, dk, dv of dt, rows dq_stride, dk_stride, dv_stride elements apart; rows of k and v that are not in use get zeros
+ *     dbias [num_buckets, heads] fp32 (NULL: not wanted), overwritten; what fs_rowwise_adagrad_update takes as `reduced` with
+ *     the bias as a table of num_buckets rows of `heads` columns
+ * work: fs_jagged_attention_backward_work_bytes(args) bytes, 16-byte aligned, contents irrelevant. */
+int fs_jagged_attention_backward(fs_ctx *ctx, const fs_attention_args *args, fs_stream stream);
+size_t fs_jagged_attention_backward_work_bytes(const fs_attention_args *args);
+
 #ifdef __cplusplus
 }
 #endif

@@ -56,6 +56,18 @@ class fs_block_args(ctypes.Structure):
     ]
 
 
+class fs_attention_args(ctypes.Structure):
+    _fields_ = [
+        ("q", c_vp), ("k", c_vp), ("v", c_vp), ("q_stride", c_i64), ("k_stride", c_i64), ("v_stride", c_i64),
+        ("n_q", c_i64), ("n_kv", c_i64), ("batch", c_i64), ("q_offsets", c_vp), ("kv_offsets", c_vp), ("kv_lengths", c_vp),
+        ("heads", c_i32), ("kv_heads", c_i32), ("head_dim", c_i32), ("dt", c_i32), ("causal", c_i32), ("max_q", c_i32),
+        ("scale", c_f), ("num_buckets", c_i32), ("num_distances", c_i32), ("bias", c_vp), ("bucket_of", c_vp),
+        ("out", c_vp), ("out_f32", c_vp), ("lse", c_vp),
+        ("dout", c_vp), ("dq", c_vp), ("dk", c_vp), ("dv", c_vp), ("dq_stride", c_i64), ("dk_stride", c_i64), ("dv_stride", c_i64),
+        ("dbias", c_vp), ("work", c_vp), ("work_bytes", ctypes.c_size_t),
+    ]
+
+
 class FreeScaleError(RuntimeError):
     def __init__(self, code: int, where: str, detail: str = ""):
         super().__init__(f"{where} failed with status {code}" + (f": {detail}" if detail else ""))
@@ -137,6 +149,10 @@ def load_library() -> ctypes.CDLL:
         "fs_block_norm": (ctypes.c_int, [c_vp, ctypes.POINTER(fs_block_args), S]),
         "fs_block_norm_backward": (ctypes.c_int, [c_vp, ctypes.POINTER(fs_block_args), S]),
         "fs_block_norm_work_bytes": (ctypes.c_size_t, [c_i64, c_i32]),
+        "fs_jagged_attention": (ctypes.c_int, [c_vp, ctypes.POINTER(fs_attention_args), S]),
+        "fs_jagged_attention_work_bytes": (ctypes.c_size_t, [ctypes.POINTER(fs_attention_args)]),
+        "fs_jagged_attention_backward": (ctypes.c_int, [c_vp, ctypes.POINTER(fs_attention_args), S]),
+        "fs_jagged_attention_backward_work_bytes": (ctypes.c_size_t, [ctypes.POINTER(fs_attention_args)]),
         "fs_init_table_hash": (ctypes.c_int, [c_vp, c_vp, c_i64, c_i32, ctypes.c_int, S]),
         "fs_stream_copy": (ctypes.c_int, [c_vp, c_vp, c_vp, c_i64, S]),
         "fs_stream_row_read": (ctypes.c_int, [c_vp, c_vp, c_i64, c_i32, c_vp, c_i64, c_vp, S]),
@@ -872,4 +888,124 @@ def fs_block_norm_backward(ctx: Context, dy: Optional[torch.Tensor], dh: Optiona
     work = _scratch(ctx, nbytes, handle)
     rec.work, rec.work_bytes = _ptr(work), work.numel()
     ctx.check(ctx.lib.fs_block_norm_backward(ctx.handle, ctypes.byref(rec), handle), "fs_block_norm_backward")
+    return res
+
+
+FS_MAX_HEAD_DIM, FS_MAX_BIAS_BUCKETS, FS_MAX_BIAS_DISTANCES = 128, 1024, 4096
+
+
+def _heads(what: str, t: torch.Tensor, shape=None, dtype=None, packed: bool = False) -> int:
+    """The row stride of a [rows, heads, head_dim] tensor whose heads lie next to each other."""
+    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {'[rows, heads, head_dim]' if shape is None else tuple(shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{what}: {t.dtype}, expected {dtype}")
+    n, heads, width = t.shape
+    if (width > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != width) or (packed and n > 1 and t.stride(0) != heads * width):
+        raise ValueError(f"{what}: strides {t.stride()}" + (", a contiguous tensor is needed" if packed else ""))
+    return t.stride(0) if n > 1 else heads * width
+
+
+def _index(what: str, t: torch.Tensor, dtype: torch.dtype, size: Optional[int] = None) -> torch.Tensor:
+    if t.dtype != dtype or t.dim() != 1 or not t.is_contiguous() or (size is not None and t.numel() != size):
+        raise ValueError(f"{what}: a contiguous {dtype} tensor" + (f" of {size} values" if size is not None else "") + " is needed")
+    return t
+
+
+def _attention_record(q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale):
+    n_q, heads, width = q.shape if q.dim() == 3 else (0, 0, 0)
+    n_kv, kv_heads = k.shape[0], k.shape[1] if k.dim() == 3 else 0
+    batch = q_offsets.numel() - 1
+    rec = fs_attention_args(
+        q=_ptr(q), k=_ptr(k), v=_ptr(v), q_stride=_heads("q", q), k_stride=_heads("k", k, (n_kv, kv_heads, width), q.dtype),
+        v_stride=_heads("v", v, (n_kv, kv_heads, width), q.dtype), n_q=n_q, n_kv=n_kv, batch=batch,
+        q_offsets=_ptr(_index("q_offsets", q_offsets, torch.int64)), heads=heads, kv_heads=kv_heads, head_dim=width,
+        kv_offsets=_ptr(_index("kv_offsets", kv_offsets, torch.int64, batch + 1)), dt=table_dtype_code(q), causal=int(causal),
+        scale=width ** -0.5 if scale is None and width else scale or 0.0)
+    if kv_lengths is not None:
+        rec.kv_lengths = _ptr(_index("kv_lengths", kv_lengths, torch.int64, batch))
+    if bias is not None:
+        if bias.dtype != torch.float32 or bias.dim() != 2 or bias.shape[1] != heads or not bias.is_contiguous():
+            raise ValueError(f"bias: a contiguous fp32 tensor [buckets, {heads}] is needed")
+        size = _index("bucket_of", bucket_of, torch.int32).numel()
+        if not causal and size % 2 == 0:
+            raise ValueError(f"bucket_of: {size} entries, an odd number is needed for distances on both sides")
+        rec.bias, rec.bucket_of, rec.num_buckets = _ptr(bias), _ptr(bucket_of), bias.shape[0]
+        rec.num_distances = size if causal else (size + 1) // 2
+    return rec
+
+
+def fs_jagged_attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
+                        kv_offsets: torch.Tensor, bias: Optional[torch.Tensor] = None, bucket_of: Optional[torch.Tensor] = None,
+                        kv_lengths: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
+                        max_q: int = 0, keep: bool = False, out: Optional[Dict[str, torch.Tensor]] = None,
+                        stream=None) -> Dict[str, torch.Tensor]:
+    """out [n_q, heads, head_dim]; keep: also what fs_jagged_attention_backward reads (lse, and out_f32 of bf16 rows).  scale:
+    1 / sqrt(head_dim) unless given.  `out`: the caller's tensors under the same names."""
+    rec = _attention_record(q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale)
+    rec.max_q = max_q
+    given, res = dict(out or {}), {}
+    shape = (rec.n_q, rec.heads, rec.head_dim)
+    wanted = {"out": q.dtype}
+    if keep or "out_f32" in given:
+        wanted["out_f32"] = torch.float32
+    for name, dt in wanted.items():
+        if name == "out_f32" and q.dtype == torch.float32:
+            continue
+        t = given[name] if name in given else torch.empty(shape, dtype=dt, device=q.device)
+        _heads(name, t, shape, dt, packed=True)
+        res[name] = t
+        setattr(rec, name, _ptr(t))
+    if keep or "lse" in given:
+        t = given["lse"] if "lse" in given else torch.empty((rec.heads, rec.n_q), dtype=torch.float32, device=q.device)
+        if t.dtype != torch.float32 or tuple(t.shape) != (rec.heads, rec.n_q) or not t.is_contiguous():
+            raise ValueError(f"lse: a contiguous fp32 tensor [{rec.heads}, {rec.n_q}] is needed")
+        res["lse"], rec.lse = t, _ptr(t)
+    _on(ctx, "fs_jagged_attention", q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, *res.values())
+    handle = _ctx_stream(ctx, stream)
+    if max_q:
+        nbytes = ctx.lib.fs_jagged_attention_work_bytes(ctypes.byref(rec))
+        if nbytes:
+            work = _scratch(ctx, nbytes, handle)
+            rec.work, rec.work_bytes = _ptr(work), work.numel()
+    ctx.check(ctx.lib.fs_jagged_attention(ctx.handle, ctypes.byref(rec), handle), "fs_jagged_attention")
+    return res
+
+
+def fs_jagged_attention_backward(ctx: Context, dout: torch.Tensor, kept: Dict[str, torch.Tensor], q: torch.Tensor, k: torch.Tensor,
+                                 v: torch.Tensor, q_offsets: torch.Tensor, kv_offsets: torch.Tensor,
+                                 bias: Optional[torch.Tensor] = None, bucket_of: Optional[torch.Tensor] = None,
+                                 kv_lengths: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
+                                 out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """dq, dk, dv, and dbias where there is a bias.  kept: what fs_jagged_attention(keep=True) returned.  `out`: the caller's
+    tensors under the same names."""
+    rec = _attention_record(q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale)
+    shape, keys = (rec.n_q, rec.heads, rec.head_dim), (rec.n_kv, rec.kv_heads, rec.head_dim)
+    _heads("dout", dout, shape, q.dtype, packed=True)
+    _heads("kept['out']", kept["out"], shape, q.dtype, packed=True)
+    rec.dout, rec.out = _ptr(dout), _ptr(kept["out"])
+    lse, exact = kept["lse"], kept.get("out_f32")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (rec.heads, rec.n_q) or not lse.is_contiguous():
+        raise ValueError(f"kept['lse']: a contiguous fp32 tensor [{rec.heads}, {rec.n_q}] is needed")
+    rec.lse = _ptr(lse)
+    if exact is not None:
+        _heads("kept['out_f32']", exact, shape, torch.float32, packed=True)
+        rec.out_f32 = _ptr(exact)
+    given, res = dict(out or {}), {}
+    for name, dims in (("dq", shape), ("dk", keys), ("dv", keys)):
+        t = given[name] if name in given else torch.empty(dims, dtype=q.dtype, device=q.device)
+        setattr(rec, name + "_stride", _heads(name, t, dims, q.dtype))
+        setattr(rec, name, _ptr(t))
+        res[name] = t
+    if bias is not None:
+        t = given["dbias"] if "dbias" in given else torch.empty_like(bias)
+        if t.dtype != torch.float32 or t.shape != bias.shape or not t.is_contiguous():
+            raise ValueError(f"dbias: a contiguous fp32 tensor {tuple(bias.shape)} is needed")
+        res["dbias"], rec.dbias = t, _ptr(t)
+    _on(ctx, "fs_jagged_attention_backward", dout, kept["out"], lse, exact, q, k, v, q_offsets, kv_offsets, bias, bucket_of,
+        kv_lengths, *res.values())
+    handle = _ctx_stream(ctx, stream)
+    work = _scratch(ctx, ctx.lib.fs_jagged_attention_backward_work_bytes(ctypes.byref(rec)), handle)
+    rec.work, rec.work_bytes = _ptr(work), work.numel()
+    ctx.check(ctx.lib.fs_jagged_attention_backward(ctx.handle, ctypes.byref(rec), handle), "fs_jagged_attention_backward")
     return res

@@ -1,0 +1,391 @@
+// What the kernels of the jagged attention share: the shapes of their tiles, how a matrix product is fed, where a workgroup
+// finds its rows, and the bias by distance.
+//
+// Products are made of 16 x 16 pieces over 32 terms.  With lane l = 16 g + j an operand piece holds, for its row (or column)
+// j, eight of the 32 terms, and which eight belong to g is a free choice as long as both operands make the same one; a result
+// piece holds column j, rows 4 g .. 4 g + 3.  Two result pieces of 16 rows each are therefore, as they lie in the registers, an
+// operand piece over their 32 rows: g has rows 4 g + i of the first and of the second.  So the scores go from the product that
+// makes them into the products that use them without a trip through LDS, in bf16 (one v_mfma_f32_16x16x32_bf16) as in fp32
+// (eight v_mfma_f32_16x16x4_f32, the i-th over element i of every g).
+#pragma once
+
+#include <type_traits>
+
+#include "fs_rowvec.h"
+
+namespace fs {
+
+constexpr int kAttnThreads = 256;
+constexpr int kAttnWaves = kAttnThreads / kWave;
+constexpr int kTile = 64;                 // keys (or query rows) of a tile in LDS
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+
+// ---- operand pieces -------------------------------------------------------------------------------------------------------
+template <typename T>
+struct piece;
+template <>
+struct piece<bf16_t> {
+    bf16x8 v;
+};
+template <>
+struct piece<float> {
+    float v[8];
+};
+
+__device__ __forceinline__ void mma(f32x4 &c, const piece<bf16_t> &a, const piece<bf16_t> &b) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x4 &c, const piece<float> &a, const piece<float> &b) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
+}
+
+// Behind the last products of a block that ends in a branch: nothing reads a result before it is there.  A matrix instruction's
+// result takes up to 10 wait states, and this compiler, which counts them out within a block, has left a copy of an accumulator
+// 3 states behind its product where a branch stood between them (fp32 rows of 32 and 64 columns: the last row of a result came
+// out one product short).
+__device__ __forceinline__ void settle() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 11");
+}
+
+// two result pieces as the operand over their rows
+__device__ __forceinline__ void as_operand(piece<bf16_t> &p, const f32x4 &lo, const f32x4 &hi) {
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x2 a = {lo[2 * i], lo[2 * i + 1]}, b = {hi[2 * i], hi[2 * i + 1]};
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2));
+        w[2 + i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(b, bf16x2));
+    }
+    p.v = __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ void as_operand(piece<float> &p, const f32x4 &lo, const f32x4 &hi) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        p.v[i] = lo[i];
+        p.v[4 + i] = hi[i];
+    }
+}
+
+// ---- tiles in LDS -------------------------------------------------------------------------------------------------------------
+// kTile rows of DH columns (the head's width rounded up to 32, 64 or 128; zeros behind it), rows 16 bytes further apart than
+// they are long: sixteen lanes that read 16 bytes each of neighbouring rows find them in different banks.
+template <typename T, int DH>
+struct tile {
+    static constexpr int kLd = DH + 16 / (int)sizeof(T);
+    static constexpr int kPer = 16 / (int)sizeof(T);              // elements of a 16-byte chunk
+    static constexpr int kChunks = DH / kPer;                     // chunks of a row
+    static constexpr int kMine = kTile * kChunks / kAttnThreads;  // chunks of a thread
+    static_assert(kMine >= 1, "a tile has at least one chunk for every thread");
+    T at[kTile * kLd];
+
+    // A over columns: rows row0 + j, columns col0 + 8 g + i
+    __device__ __forceinline__ void rows(piece<T> &p, int row0, int col0) const {
+        const int lane = threadIdx.x & 63;
+        const T *s = at + (row0 + (lane & 15)) * kLd + col0 + 8 * (lane >> 4);
+        if constexpr (sizeof(T) == 2) {
+            p.v = *reinterpret_cast<const bf16x8 *>(s);
+        } else {
+            const f32x4 a = *reinterpret_cast<const f32x4 *>(s), b = *reinterpret_cast<const f32x4 *>(s + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p.v[i] = a[i];
+                p.v[4 + i] = b[i];
+            }
+        }
+    }
+    // A over rows (the tile transposed): columns col0 + j, rows row0 + 4 g + i and row0 + 16 + 4 g + i, i < 4
+    __device__ __forceinline__ void cols(piece<T> &p, int row0, int col0) const {
+        const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+        if constexpr (sizeof(T) == 2) {
+            // the sixteen lanes of a g name four rows, four columns each, and get a column of the four rows each
+            const T *s = at + (row0 + 4 * g + (j >> 2)) * kLd + col0 + 4 * (j & 3);
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)s);
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(s + 16 * kLd));
+            const u32x2 x = __builtin_bit_cast(u32x2, a), y = __builtin_bit_cast(u32x2, b);
+            const u32x4 w = {x[0], x[1], y[0], y[1]};
+            p.v = __builtin_bit_cast(bf16x8, w);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) p.v[i] = at[(row0 + 16 * (i / 4) + 4 * g + (i & 3)) * kLd + col0 + j];
+        }
+    }
+};
+
+// a word with zeros in place of the elements that are no numbers; says whether there were any
+template <typename T>
+__device__ __forceinline__ uint32_t clean_word(uint32_t w, bool &any) {
+    const bool hi = (w & 0x7F800000u) == 0x7F800000u;
+    if constexpr (sizeof(T) == 4) {
+        any |= hi;
+        return hi ? 0u : w;
+    } else {
+        const bool lo = (w & 0x7F80u) == 0x7F80u;
+        any |= lo | hi;
+        return (lo ? 0u : w & 0xFFFFu) | (hi ? 0u : w & 0xFFFF0000u);
+    }
+}
+
+// tiles of a kind in LDS: one to work on and one to fill, but for the widest rows, of which two pairs would not fit
+template <typename T, int DH>
+constexpr int tile_buffers = sizeof(T) * DH >= 512 ? 1 : 2;
+
+// A thread's chunks of the next tile on their way from memory to LDS.
+template <typename T, int DH>
+struct tile_regs {
+    u32x4 v[tile<T, DH>::kMine];
+    // rows [0, rows) of base exist, columns [0, width)
+    __device__ __forceinline__ void load(const T *__restrict__ base, int64_t stride, int rows, int width) {
+        using t = tile<T, DH>;
+#pragma unroll
+        for (int m = 0; m < t::kMine; ++m) {
+            const int k = threadIdx.x + kAttnThreads * m, r = k / t::kChunks, c = (k % t::kChunks) * t::kPer;
+            const u32x4 zero = {0u, 0u, 0u, 0u};
+            v[m] = r < rows && c < width ? *reinterpret_cast<const u32x4 *>(base + r * stride + c) : zero;
+        }
+    }
+    __device__ __forceinline__ void store(tile<T, DH> &to) const {
+        using t = tile<T, DH>;
+#pragma unroll
+        for (int m = 0; m < t::kMine; ++m) {
+            const int k = threadIdx.x + kAttnThreads * m, r = k / t::kChunks, c = (k % t::kChunks) * t::kPer;
+            *reinterpret_cast<u32x4 *>(to.at + r * t::kLd + c) = v[m];
+        }
+    }
+    // Zeros in place of infinities and NaN; says whether this thread had any.  mark, where it is given, gets a NaN for every
+    // row that had one and a zero for every other: a row's chunks are neighbouring lanes of one wavefront.
+    __device__ __forceinline__ bool clean(float *mark = nullptr) {
+        using t = tile<T, DH>;
+        bool any = false;
+#pragma unroll
+        for (int m = 0; m < t::kMine; ++m) {
+            bool mine = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[m][i] = clean_word<T>(v[m][i], mine);
+            any |= mine;
+            if (mark) {
+                const int k = threadIdx.x + kAttnThreads * m, lane = threadIdx.x & 63;
+                const uint64_t row = (__ballot(mine) >> (lane & ~(t::kChunks - 1))) & ((1ull << t::kChunks) - 1);
+                if (k % t::kChunks == 0) mark[k / t::kChunks] = row ? __builtin_nanf("") : 0.f;
+            }
+        }
+        return any;
+    }
+};
+
+__device__ __forceinline__ float load1(const float *p) { return *p; }
+__device__ __forceinline__ float load1(const bf16_t *p) { return __uint_as_float((uint32_t)p->bits << 16); }
+
+// An operand over columns straight from memory: rows j of base (rows [0, rows) exist), columns col0 + 8 g + i below width.
+template <typename T>
+__device__ __forceinline__ void global_rows(piece<T> &p, const T *__restrict__ base, int64_t stride, int row, bool live, int col0,
+                                            int width) {
+    const int col = col0 + 8 * ((threadIdx.x & 63) >> 4);
+    const T *s = base + row * stride + col;
+    const u32x4 zero = {0u, 0u, 0u, 0u};
+    if constexpr (sizeof(T) == 2) {
+        p.v = __builtin_bit_cast(bf16x8, live && col < width ? *reinterpret_cast<const u32x4 *>(s) : zero);
+    } else {
+        const u32x4 a = live && col < width ? *reinterpret_cast<const u32x4 *>(s) : zero;
+        const u32x4 b = live && col + 4 < width ? *reinterpret_cast<const u32x4 *>(s + 4) : zero;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p.v[i] = __uint_as_float(a[i]);
+            p.v[4 + i] = __uint_as_float(b[i]);
+        }
+    }
+}
+
+// Four neighbouring columns of a result row (result pieces hold rows of the transposed product).
+__device__ __forceinline__ void store4(float *p, const f32x4 &v) { *reinterpret_cast<f32x4 *>(p) = v; }
+__device__ __forceinline__ void store4(bf16_t *p, const f32x4 &v) {
+    u32x2 w;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x2 a = {v[2 * i], v[2 * i + 1]};
+        w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(a, bf16x2));
+    }
+    *reinterpret_cast<u32x2 *>(p) = w;
+}
+
+// sum and maximum over the four g of a column, in every one of them
+__device__ __forceinline__ float column_sum(float x) {
+    const unsigned u = __float_as_uint(x);
+    const u32x2 a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const unsigned v = __float_as_uint(y);
+    const u32x2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+__device__ __forceinline__ float column_max(float x) {
+    const unsigned u = __float_as_uint(x);
+    const u32x2 a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const unsigned v = __float_as_uint(y);
+    const u32x2 b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// ---- where the rows are -----------------------------------------------------------------------------------------------------
+struct attn_params {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    int64_t n_q, n_kv, batch;
+    const int64_t *q_offsets, *kv_offsets, *kv_lengths;
+    int heads, group, width, causal;         // group: query heads that share a key head
+    float scale;
+    const float *bias;                       // [buckets, heads], or NULL
+    const int32_t *bucket_of;
+    int buckets, distances;                  // distances behind the last are the last
+    void *out;
+    float *out_f32, *lse;                    // lse [heads, n_q]
+    const void *dout;
+    void *dq, *dk, *dv;
+    int64_t dq_stride, dk_stride, dv_stride;
+    float *dbias;
+    float *delta;                            // scratch [heads, n_q]
+    float *bias_part;                        // scratch [slots, heads, buckets]
+    float *split_acc, *split_ml;             // scratch of the split form
+    int split_shift, max_q;
+    int *flags;
+};
+
+struct user {
+    int64_t q0, k0;                          // first row of its queries, of its keys
+    int64_t b;
+    int nq, nk;                              // how many of each
+    int room;                                // rows of k and v that are the user's, the unused ones among them
+    int first;                               // position of its first query row among its keys: nk - nq, may be negative
+};
+
+// Slots: tiles of 2^shift rows of one user, numbered so that a user's begin at offsets[b] / 2^shift + b, which leaves room for
+// one that is cut off at each end and needs nobody to add up the tiles before.  Finds the user of a slot (a 64-ary search by
+// the whole wavefront) and which of its tiles the slot is; false where there is none.  Boundaries that do not fit are flagged
+// and their user left out; every access stays inside the rows whatever the offsets hold.
+__device__ __forceinline__ bool find_user(const attn_params &p, const int64_t *__restrict__ offsets, int64_t slot, int shift, user &u,
+                                          int &index) {
+    const int lane = threadIdx.x & 63;
+    int64_t lo = 0, hi = p.batch - 1;        // user lo begins at or before the slot (or there is no such user)
+    while (lo < hi) {
+        const int64_t step = (hi - lo + 63) / 64;
+        const int64_t probe = lo + (lane + 1) * step;
+        const bool le = probe <= hi && (offsets[probe] >> shift) + probe <= slot;
+        const int cnt = __popcll(__ballot(le));
+        const int64_t nhi = lo + (cnt + 1) * step - 1;
+        lo += cnt * step;
+        hi = nhi < hi ? nhi : hi;
+        hi = hi < lo ? lo : hi;
+    }
+    u.b = lo;
+    const int64_t qa = p.q_offsets[lo], qb = p.q_offsets[lo + 1], ka = p.kv_offsets[lo], kb = p.kv_offsets[lo + 1];
+    if (qa < 0 || qb < qa || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv || qb - qa > 0x3fffffff || kb - ka > 0x3fffffff)
+        return false;
+    u.q0 = qa;
+    u.k0 = ka;
+    u.nq = (int)(qb - qa);
+    u.nk = u.room = (int)(kb - ka);
+    if (p.kv_lengths) {
+        const int64_t used = p.kv_lengths[lo];
+        u.nk = used < 0 ? 0 : used < u.nk ? (int)used : u.nk;
+    }
+    u.first = u.nk - u.nq;
+    const int64_t k = slot - ((offsets[lo] >> shift) + lo);
+    index = (int)k;
+    return k >= 0 && k < 0x3fffffff;
+}
+
+// Thread by thread over the whole grid: offsets that do not ascend from 0 to the number of rows, lengths beyond their room.
+__device__ __forceinline__ void check_layout(const attn_params &p, int64_t group) {
+    for (int64_t b = group * kAttnThreads + threadIdx.x; b < p.batch; b += (int64_t)gridDim.x * kAttnThreads) {
+        const int64_t qa = p.q_offsets[b], qb = p.q_offsets[b + 1], ka = p.kv_offsets[b], kb = p.kv_offsets[b + 1];
+        bool bad = qa < 0 || qb < qa || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv;
+        bad |= b == 0 && (qa != 0 || ka != 0);
+        bad |= b == p.batch - 1 && (qb != p.n_q || kb != p.n_kv);
+        bad |= qb - qa > 0x3fffffff || kb - ka > 0x3fffffff;
+        if (p.kv_lengths) bad |= p.kv_lengths[b] < 0 || p.kv_lengths[b] > kb - ka;
+        if (bad) atomicOr(p.flags, kFlagOffsets);
+    }
+}
+
+// ---- the bias by distance -----------------------------------------------------------------------------------------------------
+// at[zero + d] is the bias of distance d (times log2 e) for the distances a workgroup meets, kPad further on either side: the
+// distances of a tile lie within kPad of one that counts, so that nobody has to bring a distance into range.
+template <int kPad>
+struct strip {
+    float *at;              // LDS
+    int zero, low, high;    // distances below low are low, above high are high; at[] begins at distance low - kPad
+
+    static __host__ __device__ int entries(int distances, bool causal) {
+        return (causal ? distances : 2 * distances - 1) + 2 * kPad;
+    }
+    // Distances from `from` to `to` (and kPad around) are met.  buckets: also which bucket each distance has, or -1.
+    // Returns whether any bias of them hides (is -inf); has a barrier.
+    __device__ __forceinline__ bool fill(const attn_params &p, int head, float *lds, int from, int to, int16_t *bucket) {
+        at = lds;
+        high = p.distances - 1;
+        low = p.causal ? 0 : -high;
+        zero = kPad - low;
+        int a = (from < low ? low : from > high ? high : from) - kPad, b = (to > high ? high : to < low ? low : to) + kPad;
+        bool hides = false;
+        for (int d = a + (int)threadIdx.x; d <= b; d += kAttnThreads) {
+            const int c = d < low ? low : d > high ? high : d;
+            float x = 0.f;
+            int k = -1;
+            if (p.bias) {
+                k = p.bucket_of[c - low];
+                if (k < 0 || k >= p.buckets) {
+                    atomicOr(p.flags, kFlagRowRange);
+                    k = -1;
+                } else {
+                    x = p.bias[(int64_t)k * p.heads + head] * kLog2e;
+                }
+            }
+            at[zero + d] = x;
+            if (bucket) bucket[zero + d] = (int16_t)k;
+            hides |= x == neg_inf();
+        }
+        return __syncthreads_or(hides) != 0;
+    }
+};
+
+// ---- host side --------------------------------------------------------------------------------------------------------------
+constexpr int kMaxLds = 160 * 1024;
+constexpr int kFreeLds = 64 * 1024;           // what a kernel may ask for without saying so beforehand
+
+template <typename F>
+int launch_attention(fs_ctx *ctx, F *kernel, int64_t groups, size_t lds, hipStream_t s, const char *name, const attn_params &p) {
+    if (lds > (size_t)kMaxLds) return set_err(ctx, FS_EINVAL, "jagged attention: head_dim, buckets and distances do not fit together");
+    if (lds > (size_t)kFreeLds)
+        FS_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+    kernel<<<(unsigned)groups, kAttnThreads, lds, s>>>(p);
+    FS_LAUNCH_CHECK(ctx, name);
+    return FS_OK;
+}
+
+// f(T *, DH) for a type and a head's width rounded up
+template <typename F>
+int by_head(int dt, int width, F &&f) {
+    const auto widths = [&](auto *t) {
+        if (width <= 32) return f(t, std::integral_constant<int, 32>());
+        if (width <= 64) return f(t, std::integral_constant<int, 64>());
+        return f(t, std::integral_constant<int, 128>());
+    };
+    return dt == FS_F32 ? widths((float *)nullptr) : widths((bf16_t *)nullptr);
+}
+
+// slots of tiles of 2^shift rows (find_user)
+inline int64_t attn_slots(int64_t rows, int64_t batch, int shift) { return (rows >> shift) + batch; }
+
+int launch_attention_backward(fs_ctx *ctx, const attn_params &p, int dt, void *work, hipStream_t s);
+size_t attention_backward_work(const attn_params &p);
+
+}  // namespace fs

@@ -1,0 +1,561 @@
+// Attention over a jagged batch with a learned relative position bias, backward.
+//
+// With P the softmax as the forward pass left it (its row sums are in lse) and D_i = dO_i . o_i:
+//   dS = P (dO V^T - D),  dq = scale dS k,  dk = scale dS^T q,  dv = P^T dO,  dbias[b, head] = sum of dS over the pairs in b
+// Two launches recompute the scores, one that owns query rows (dq, D and the bias) and one that owns keys (dk, dv): seven
+// products instead of the five of a single launch, and in exchange no sum crosses a workgroup but the bias's, so that nothing
+// is added up in an order that changes.  Both keep the scores in registers from product to product, as the forward pass does.
+#include "fs_attention.h"
+
+using namespace fs;
+
+namespace {
+
+// ---- the bias's gradient ------------------------------------------------------------------------------------------------------
+// A wavefront's sums by bucket, in LDS that only it writes.
+struct bucket_sums {
+    float *bins;            // [buckets]
+    float run = 0.f;        // a lane's share of the bucket below, not yet in its bin
+    int now = -1;
+
+    static __device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+        for (int m = 1; m < kWave; m <<= 1) x += __shfl_xor(x, m, kWave);
+        return x;
+    }
+    __device__ __forceinline__ void add(int bucket, float total) {       // of the whole wavefront
+        if (bucket >= 0 && (threadIdx.x & 63) == 0) bins[bucket] += total;
+    }
+    __device__ __forceinline__ void flush() {
+        add(now, wave_sum(run));
+        run = 0.f;
+    }
+    // every lane's share of one bucket
+    __device__ __forceinline__ void one(int bucket, float share) {
+        if (bucket != now) {
+            flush();
+            now = bucket;
+        }
+        run += share;
+    }
+    // every lane's value of a bucket of its own: bucket after bucket
+    __device__ __forceinline__ void each(int bucket, float value) {
+        uint64_t left = __ballot(bucket >= 0);
+        while (left) {
+            const int b = __builtin_amdgcn_readlane(bucket, __ffsll((unsigned long long)left) - 1);
+            const bool mine = bucket == b;
+            add(b, wave_sum(mine ? value : 0.f));
+            left &= ~__ballot(mine);
+        }
+    }
+};
+
+// A wavefront's 16 query rows x 64 keys, summed along its diagonals: value (q, key) belongs to distance q - key + 63 of the
+// 79.  Each value is written where its distance's row has column q; a row then has at most 16, and rows d and d + 64 share
+// them: row d has columns up to d, row d + 64 those behind.
+constexpr int kSkewLd = 17;
+constexpr int kSkew = (kTile + 15) * kSkewLd;
+__device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], float &near, float &far) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) skew[(j + 63 - 16 * k - 4 * g - r) * kSkewLd + j] = s[k][r];
+    wave_lds_order();
+    near = far = 0.f;
+    const float *row = skew + lane * kSkewLd;
+    const int cut = lane < 15 ? lane : 15;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+        const float x = row[q + (q > cut ? 64 * kSkewLd : 0)];
+        if (q <= cut) near += x;
+        else far += x;
+    }
+    wave_lds_order();
+}
+
+// ---- query rows ---------------------------------------------------------------------------------------------------------------
+template <typename T, int DH>
+__global__ __launch_bounds__(kAttnThreads) void attn_dq_kernel(attn_params p) {
+    constexpr int kRows = 16 * kAttnWaves, kShift = 6, kPad = kRows + kTile;
+    constexpr int KC = DH / 32, MT = DH / 16;
+    extern __shared__ __align__(16) char lds[];
+    constexpr int kBufs = tile_buffers<T, DH>;
+    tile<T, DH> *kt = reinterpret_cast<tile<T, DH> *>(lds), *vt = kt + kBufs;
+    float *mark = reinterpret_cast<float *>(vt + kBufs);                              // [2][kTile]
+    float *skew = mark + 2 * kTile;                                               // [wavefronts][kSkew]
+    float *bias_lds = skew + kAttnWaves * kSkew;
+    const int entries = strip<kPad>::entries(p.distances, p.causal != 0);
+    float *bins = bias_lds + entries;                                             // [wavefronts][buckets]
+    int16_t *bucket_lds = reinterpret_cast<int16_t *>(bins + kAttnWaves * p.buckets);
+
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
+    const int head = blockIdx.x % p.heads;
+    const int64_t slot = blockIdx.x / p.heads;
+    if (head == 0) check_layout(p, slot);
+    user u;
+    int index;
+    float *part = p.dbias ? p.bias_part + (slot * p.heads + head) * p.buckets : nullptr;
+    if (!find_user(p, p.q_offsets, slot, kShift, u, index) || (int64_t)index * kRows >= u.nq) {
+        if (part)
+            for (int b = threadIdx.x; b < p.buckets; b += kAttnThreads) part[b] = 0.f;
+        return;
+    }
+    const int row0 = index * kRows;
+    const int rows = u.nq - row0 < kRows ? u.nq - row0 : kRows;
+    const int pos0 = u.first + row0, pos_last = pos0 + rows - 1;
+    const int end = p.causal ? (pos_last + 1 < u.nk ? pos_last + 1 : u.nk) : u.nk;
+    const int tiles = end <= 0 ? 0 : (end + kTile - 1) / kTile;
+    const T *kbase = static_cast<const T *>(p.k) + u.k0 * p.k_stride + (head / p.group) * p.width;
+    const T *vbase = static_cast<const T *>(p.v) + u.k0 * p.v_stride + (head / p.group) * p.width;
+
+    tile_regs<T, DH> kr, vr;
+    kr.load(kbase, p.k_stride, tiles ? u.nk : 0, p.width);
+    vr.load(vbase, p.v_stride, tiles ? u.nk : 0, p.width);
+
+    const int wrow = row0 + 16 * w, wpos = u.first + wrow, row = wrow + j;
+    const bool live = row < u.nq;
+    piece<T> qf[KC], of[KC];
+    const int64_t orow = p.heads * (int64_t)p.width;                              // out and dout are packed
+    const int64_t obase = u.q0 * orow + head * p.width;
+    float delta = 0.f;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+        global_rows(qf[c], static_cast<const T *>(p.q) + u.q0 * p.q_stride + head * p.width, p.q_stride, row, live, 32 * c, p.width);
+        global_rows(of[c], static_cast<const T *>(p.dout) + obase, orow, row, live, 32 * c, p.width);
+        const int col = 32 * c + 8 * g, left = live ? p.width - col : 0;
+        const int64_t at = obase + row * orow + col;
+        float o[8], d[8];
+        if (p.out_f32) load8(p.out_f32 + at, left, o);
+        else load8(static_cast<const T *>(p.out) + at, left, o);
+        load8(static_cast<const T *>(p.dout) + at, left, d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) delta += o[i] * d[i];
+    }
+    delta = column_sum(delta);
+    float lse2 = __builtin_inff();                                                // a row that sees nothing: P = 0
+    if (live) {
+        const int64_t at = (int64_t)head * p.n_q + u.q0 + row;
+        const float x = p.lse[at];
+        if (x != neg_inf()) lse2 = x * kLog2e;
+        if (g == 0) p.delta[at] = delta;
+    }
+    strip<kPad> bias;
+    bucket_sums sums;
+    sums.bins = bins + w * p.buckets;
+    if (part)
+        for (int b = lane; b < p.buckets; b += kWave) sums.bins[b] = 0.f;
+    const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last, part ? bucket_lds : nullptr);
+    const float scale2 = p.scale * kLog2e;
+
+    f32x4 acc[MT] = {};
+    // some rows do not see all keys of the tile, or some of those are none
+    const auto edge = [&](int n) { return hides || (n + 1) * kTile > u.nk || (p.causal && (n + 1) * kTile - 1 > pos0); };
+    const auto stage = [&](int n) {
+        // what a row does not see must not reach it, not even as 0 * NaN: the keys' infinities and NaN are taken out of the
+        // product and put into the scores, where they are masked like any other
+        if (kBufs == 1) __syncthreads();
+        if (edge(n)) kr.clean(mark + (n & 1) * kTile);
+        kr.store(kt[n & (kBufs - 1)]);
+        vr.store(vt[n & (kBufs - 1)]);
+    };
+    if (tiles) stage(0);
+    for (int n = 0; n < tiles; ++n) {
+        __syncthreads();
+        const int key0 = n * kTile;
+        if (n + 1 < tiles) {
+            kr.load(kbase + (int64_t)(key0 + kTile) * p.k_stride, p.k_stride, u.nk - key0 - kTile, p.width);
+            vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile, p.width);
+        }
+        const tile<T, DH> &K = kt[n & (kBufs - 1)], &V = vt[n & (kBufs - 1)];
+        if (wrow < u.nq && !(p.causal && key0 > wpos + 15)) {
+            f32x4 s[4], dp[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                s[k] = dp[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < KC; ++c) {
+                    piece<T> a;
+                    K.rows(a, 16 * k, 32 * c);
+                    mma(s[k], a, qf[c]);
+                    V.rows(a, 16 * k, 32 * c);
+                    mma(dp[k], a, of[c]);
+                }
+            }
+            const int nearest = wpos - (key0 + kTile - 1), furthest = wpos + 15 - key0;
+            const bool all_far = nearest >= bias.high || furthest <= bias.low;
+            const int far_at = bias.zero + (nearest >= bias.high ? bias.high : bias.low);
+            const float far = bias.at[far_at];
+            const float *bb = bias.at + bias.zero + (wpos + j - key0 - 4 * g) - 51;
+            const auto score = [&](auto mask) {
+                const int seen = p.causal ? min(wpos + j + 1, u.nk) : u.nk;          // keys that the row sees
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    f32x4 x;
+                    if constexpr (mask()) x = *reinterpret_cast<const f32x4 *>(mark + (n & 1) * kTile + 16 * k + 4 * g);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float b = all_far ? far : bb[51 - 16 * k - r];
+                        float power = s[k][r] * scale2 + b - lse2, d = dp[k][r] - delta;
+                        if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen ? power + x[r] : neg_inf();
+                        const float e = __builtin_amdgcn_exp2f(power);
+                        if constexpr (mask()) d = e == 0.f ? 0.f : d;
+                        s[k][r] = e * d;
+                    }
+                }
+            };
+            if (edge(n)) score(std::true_type());
+            else score(std::false_type());
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                piece<T> sf;
+                as_operand(sf, s[2 * c], s[2 * c + 1]);
+#pragma unroll
+                for (int d = 0; d < MT; ++d) {
+                    piece<T> a;
+                    K.cols(a, 32 * c, 16 * d);
+                    mma(acc[d], a, sf);
+                }
+            }
+            settle();
+            if (part) {
+                int b0 = 0, b1 = 0;
+                bool same = all_far;
+                if (!all_far) {
+                    const int16_t *b = bucket_lds + bias.zero + nearest;          // buckets of the 79 distances
+                    b0 = b[lane];
+                    b1 = lane < 15 ? b[64 + lane] : b0;
+                    const int first = __builtin_amdgcn_readfirstlane(b0);
+                    same = __all(b0 == first && b1 == first);
+                }
+                if (same) {
+                    float share = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) share += (s[k][0] + s[k][1]) + (s[k][2] + s[k][3]);
+                    sums.one(all_far ? bucket_lds[far_at] : __builtin_amdgcn_readfirstlane(b0), share);
+                } else {
+                    float near, far;
+                    diagonal_sums(skew + w * kSkew, s, near, far);
+                    sums.each(b0, near);
+                    sums.each(lane < 15 ? b1 : -1, far);
+                }
+            }
+        }
+        if (n + 1 < tiles) stage(n + 1);
+    }
+    if (live) {
+#pragma unroll
+        for (int c = 0; c < MT; ++c) {
+            const int col = 16 * c + 4 * g;
+            f32x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = acc[c][r] * p.scale;
+            if (col < p.width) store4(static_cast<T *>(p.dq) + (u.q0 + row) * p.dq_stride + head * p.width + col, o);
+        }
+    }
+    if (part) {
+        sums.flush();
+        __syncthreads();
+        for (int b = threadIdx.x; b < p.buckets; b += kAttnThreads) {
+            float x = 0.f;
+#pragma unroll
+            for (int v = 0; v < kAttnWaves; ++v) x += bins[v * p.buckets + b];
+            part[b] = x;
+        }
+    }
+}
+
+// ---- keys ------------------------------------------------------------------------------------------------------------------------
+// KT: sixteens of keys of a wavefront
+template <typename T, int DH, int KT>
+__global__ __launch_bounds__(kAttnThreads) void attn_dkv_kernel(attn_params p) {
+    constexpr int kKeys = 16 * kAttnWaves * KT, kShift = KT == 1 ? 6 : 7, kPad = kKeys + kTile;
+    constexpr int KC = DH / 32, MT = DH / 16;
+    extern __shared__ __align__(16) char lds[];
+    constexpr int kBufs = tile_buffers<T, DH>;
+    tile<T, DH> *qt = reinterpret_cast<tile<T, DH> *>(lds), *ot = qt + kBufs;
+    float *stats = reinterpret_cast<float *>(ot + kBufs);                         // [2][lse, delta][kTile]
+    float *mark = stats + 4 * kTile;                                              // [2][q, dout][kTile]
+    uint32_t *odd = reinterpret_cast<uint32_t *>(mark + 4 * kTile);               // [2][wavefronts]
+    float *bias_lds = reinterpret_cast<float *>(odd + 2 * kAttnWaves);
+
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
+    const int kv_heads = p.heads / p.group, kvh = blockIdx.x % kv_heads;
+    user u;
+    int index;
+    if (!find_user(p, p.kv_offsets, blockIdx.x / kv_heads, kShift, u, index) || (int64_t)index * kKeys >= u.room) return;
+    const int key_first = index * kKeys;
+    const int wkey = key_first + 16 * KT * w;
+    // query rows at or behind the first key; every tile of 64 of them, for every head that shares the keys
+    const int from = p.causal && key_first > u.first ? (key_first - u.first) / kTile * kTile : 0;
+    const int tiles = key_first >= u.nk || from >= u.nq ? 0 : (u.nq - from + kTile - 1) / kTile;
+    const int turns = tiles * p.group;
+
+    piece<T> kf[KT][KC], vf[KT][KC];
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+        const int key = wkey + 16 * t + j;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            global_rows(kf[t][c], static_cast<const T *>(p.k) + u.k0 * p.k_stride + kvh * p.width, p.k_stride, key, key < u.nk, 32 * c,
+                        p.width);
+            global_rows(vf[t][c], static_cast<const T *>(p.v) + u.k0 * p.v_stride + kvh * p.width, p.v_stride, key, key < u.nk, 32 * c,
+                        p.width);
+        }
+    }
+    f32x4 dk[KT][MT] = {}, dv[KT][MT] = {};
+    const int64_t orow = p.heads * (int64_t)p.width;
+    const float scale2 = p.scale * kLog2e;
+    tile_regs<T, DH> qr, dr;
+    float stat = 0.f;
+    const auto fetch = [&](int n) {
+        const int head = kvh * p.group + n / tiles, r0 = from + (n % tiles) * kTile;
+        qr.load(static_cast<const T *>(p.q) + (u.q0 + r0) * p.q_stride + head * p.width, p.q_stride, u.nq - r0, p.width);
+        dr.load(static_cast<const T *>(p.dout) + (u.q0 + r0) * orow + head * p.width, orow, u.nq - r0, p.width);
+        if (threadIdx.x < 2 * kTile) {
+            const int r = r0 + (threadIdx.x & (kTile - 1));
+            const bool lse = threadIdx.x < kTile;
+            stat = lse ? __builtin_inff() : 0.f;                                  // rows that see nothing and rows that are none
+            if (r < u.nq) {
+                const float x = (lse ? p.lse : p.delta)[(int64_t)head * p.n_q + u.q0 + r];
+                if (!lse) stat = x;
+                else if (x != neg_inf()) stat = x * kLog2e;
+            }
+        }
+    };
+    strip<kPad> bias;
+    bool hides = false;
+    // some of the tile's rows do not see all keys of the workgroup, or some of those are none
+    const auto edge = [&](int n) {
+        return key_first + kKeys > u.nk || (p.causal && u.first + from + (n % tiles) * kTile < key_first + kKeys - 1);
+    };
+    const auto stage = [&](int n, bool clean) {
+        const int b = n & 1;
+        if (kBufs == 1) __syncthreads();
+        if (clean) {
+            qr.clean(mark + (2 * b) * kTile);
+            const bool any = __any(dr.clean(mark + (2 * b + 1) * kTile));
+            if (lane == 0) odd[b * kAttnWaves + w] = any;
+        }
+        qr.store(qt[n & (kBufs - 1)]);
+        dr.store(ot[n & (kBufs - 1)]);
+        if (threadIdx.x < 2 * kTile) stats[2 * b * kTile + threadIdx.x] = stat;
+    };
+    const auto fill = [&](int n) {
+        return bias.fill(p, kvh * p.group + n / tiles, bias_lds, u.first + from - (key_first + kKeys - 1), u.first + u.nq - 1 - key_first,
+                         nullptr);
+    };
+    bool masked = false;                      // the tile at hand was cleaned, and is worked on with its marks and masks
+    if (turns > 0) {
+        fetch(0);
+        hides = fill(0);
+        stage(0, masked = edge(0) || hides);
+    }
+    for (int n = 0; n < turns; ++n) {
+        __syncthreads();
+        if (n > 0 && n % tiles == 0) hides = fill(n);
+        const int b = n & 1, r0 = from + (n % tiles) * kTile, pos0 = u.first + r0, head = kvh * p.group + n / tiles;
+        if (n + 1 < turns) fetch(n + 1);
+        const tile<T, DH> &Q = qt[n & (kBufs - 1)], &O = ot[n & (kBufs - 1)];
+        if (wkey < u.nk && !(p.causal && pos0 + kTile - 1 < wkey)) {
+#pragma unroll
+            for (int c2 = 0; c2 < 2; ++c2) {                                      // 32 query rows at a time
+                if (r0 + 32 * c2 >= u.nq) break;
+                f32x4 s[2][KT], dp[2][KT];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) s[h][t] = dp[h][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) {
+                        piece<T> a;
+                        Q.rows(a, 32 * c2 + 16 * h, 32 * c);
+#pragma unroll
+                        for (int t = 0; t < KT; ++t) mma(s[h][t], a, kf[t][c]);
+                        O.rows(a, 32 * c2 + 16 * h, 32 * c);
+#pragma unroll
+                        for (int t = 0; t < KT; ++t) mma(dp[h][t], a, vf[t][c]);
+                    }
+                }
+                // element r of s[h][t]: query row r0 + 32 c2 + 16 h + 4 g + r, key wkey + 16 t + j
+                const int nearest = pos0 + 32 * c2 - (wkey + 16 * KT - 1), furthest = pos0 + 32 * c2 + 31 - wkey;
+                const bool all_far = nearest >= bias.high || furthest <= bias.low;
+                const float far = bias.at[bias.zero + (nearest >= bias.high ? bias.high : bias.low)];
+                const float *bb = bias.at + bias.zero + (pos0 + 32 * c2 + 4 * g - wkey - j) - 16 * (KT - 1);
+                const auto score = [&](auto mask) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int at = 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
+                        const f32x4 lse = *reinterpret_cast<const f32x4 *>(stats + at);
+                        const f32x4 delta = *reinterpret_cast<const f32x4 *>(stats + kTile + at);
+                        f32x4 mq, mo;
+                        if constexpr (mask()) {
+                            mq = *reinterpret_cast<const f32x4 *>(mark + at);
+                            mo = *reinterpret_cast<const f32x4 *>(mark + kTile + at);
+                        }
+#pragma unroll
+                        for (int t = 0; t < KT; ++t)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                const float x = all_far ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
+                                float power = s[h][t][r] * scale2 + x - lse[r], d = dp[h][t][r] - delta[r];
+                                if constexpr (mask()) {
+                                    // a key that the row does not see, and the keys behind the last
+                                    const int key = wkey + 16 * t + j;
+                                    const int seen = p.causal ? min(pos0 + 32 * c2 + 16 * h + 4 * g + r + 1, u.nk) : u.nk;
+                                    power = key < seen ? power + mq[r] : neg_inf();
+                                    d += mo[r];
+                                }
+                                const float e = __builtin_amdgcn_exp2f(power);
+                                if constexpr (mask()) d = e == 0.f ? 0.f : d;
+                                s[h][t][r] = e;
+                                dp[h][t][r] = e * d;
+                            }
+                    }
+                };
+                if (masked) score(std::true_type());
+                else score(std::false_type());
+#pragma unroll
+                for (int t = 0; t < KT; ++t) {
+                    piece<T> pf, sf;
+                    as_operand(pf, s[0][t], s[1][t]);
+                    as_operand(sf, dp[0][t], dp[1][t]);
+#pragma unroll
+                    for (int d = 0; d < MT; ++d) {
+                        piece<T> a;
+                        O.cols(a, 32 * c2, 16 * d);
+                        mma(dv[t][d], a, pf);
+                        Q.cols(a, 32 * c2, 16 * d);
+                        mma(dk[t][d], a, sf);
+                    }
+                }
+                settle();
+            }
+            if (masked) {
+                uint32_t any = 0;
+                for (int x = 0; x < kAttnWaves; ++x) any |= odd[b * kAttnWaves + x];
+                if (any) {
+                    // the elements of dout left out of the product, row by row, for the keys that are seen
+                    const int count = u.nq - r0 < kTile ? u.nq - r0 : kTile;
+                    for (int q = 0; q < count; ++q) {
+                        const T *o = static_cast<const T *>(p.dout) + (u.q0 + r0 + q) * orow + head * p.width;
+#pragma unroll
+                        for (int t = 0; t < KT; ++t) {
+                            const int key = wkey + 16 * t + j, d = pos0 + q - key;
+                            const int dc = d > bias.high ? bias.high : d < bias.low ? bias.low : d;
+                            const bool sees = key < u.nk && !(p.causal && d < 0) && bias.at[bias.zero + dc] != neg_inf();
+#pragma unroll
+                            for (int c = 0; c < MT; ++c)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r) {
+                                    const int col = 16 * c + 4 * g + r;
+                                    const float x = col < p.width ? load1(o + col) : 0.f;
+                                    if (sees && !(fabsf(x) < __builtin_inff())) dv[t][c][r] += x;
+                                }
+                        }
+                    }
+                }
+            }
+        }
+        if (n + 1 < turns) {
+            // a head's first tile is put down before its bias is known to hide nothing
+            masked = edge(n + 1) || hides || (n + 1) % tiles == 0;
+            stage(n + 1, masked);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < KT; ++t) {
+        const int key = wkey + 16 * t + j;
+        if (key >= u.room) continue;
+#pragma unroll
+        for (int c = 0; c < MT; ++c) {
+            const int col = 16 * c + 4 * g;
+            if (col >= p.width) continue;
+            f32x4 o;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o[r] = dk[t][c][r] * p.scale;
+            store4(static_cast<T *>(p.dk) + (u.k0 + key) * p.dk_stride + kvh * p.width + col, o);
+            store4(static_cast<T *>(p.dv) + (u.k0 + key) * p.dv_stride + kvh * p.width + col, dv[t][c]);
+        }
+    }
+}
+
+// ---- the bias's gradient, added up over the workgroups ---------------------------------------------------------------------------
+// [slots, columns] in two launches, 64 columns a workgroup: kBiasCuts cuts of the slots into sums of 64 bits, then those.
+constexpr int kBiasCuts = 64;
+__global__ __launch_bounds__(256) void attn_bias_cut_kernel(const float *__restrict__ part, int64_t slots, int columns,
+                                                            double *__restrict__ cut) {
+    __shared__ double sh[4][64];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
+    const int64_t per = (slots + kBiasCuts - 1) / kBiasCuts, a = blockIdx.y * per, b = a + per < slots ? a + per : slots;
+    double s = 0.0;
+    if (c < columns)
+        for (int64_t k = a + w; k < b; k += 4) s += (double)part[k * columns + c];
+    sh[w][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (w == 0 && c < columns) cut[(int64_t)blockIdx.y * columns + c] = (sh[0][c & 63] + sh[1][c & 63]) + (sh[2][c & 63] + sh[3][c & 63]);
+}
+__global__ __launch_bounds__(256) void attn_bias_sum_kernel(const double *__restrict__ cut, int heads, int buckets, int cuts,
+                                                            float *__restrict__ dbias) {
+    const int k = blockIdx.x * 256 + threadIdx.x, columns = heads * buckets;
+    if (k >= columns) return;
+    const int head = k % heads, bucket = k / heads;
+    double s = 0.0;
+    for (int c = 0; c < cuts; ++c) s += cut[(int64_t)c * columns + head * buckets + bucket];
+    dbias[k] = (float)s;
+}
+
+// keys of a wavefront: twice sixteen halve what a score reads from LDS; fp32 and the widest rows have no registers for them
+template <typename T, int DH>
+constexpr int key_sixteens = sizeof(T) == 2 && DH <= 64 ? 2 : 1;
+
+}  // namespace
+
+namespace fs {
+
+// scratch: delta, then the bias's sums of every workgroup, then those of the cuts
+static size_t delta_bytes(const attn_params &p) { return ((size_t)p.heads * p.n_q * sizeof(float) + 255) / 256 * 256; }
+static size_t part_bytes(const attn_params &p) {
+    if (!p.dbias) return 0;
+    return ((size_t)attn_slots(p.n_q, p.batch, 6) * p.heads * p.buckets * sizeof(float) + 255) / 256 * 256;
+}
+
+size_t attention_backward_work(const attn_params &p) {
+    return delta_bytes(p) + part_bytes(p) + (p.dbias ? (size_t)kBiasCuts * p.heads * p.buckets * sizeof(double) : 0);
+}
+
+int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void *work, hipStream_t s) {
+    attn_params p = args;
+    p.delta = static_cast<float *>(work);
+    p.bias_part = reinterpret_cast<float *>(static_cast<char *>(work) + delta_bytes(p));
+    double *cut = reinterpret_cast<double *>(static_cast<char *>(work) + delta_bytes(p) + part_bytes(p));
+    const int64_t slots = attn_slots(p.n_q, p.batch, 6);
+    const bool causal = p.causal != 0;
+    if (p.batch > 0) {
+        const int rc = by_head(dt, p.width, [&](auto *t, auto dh) -> int {
+            using T = std::remove_pointer_t<decltype(t)>;
+            constexpr int DH = dh(), KT = key_sixteens<T, DH>, B = tile_buffers<T, DH>;
+            const size_t bias = strip<16 * kAttnWaves + kTile>::entries(p.distances, causal);
+            const size_t rows = 2 * B * sizeof(tile<T, DH>) + (2 * kTile + kAttnWaves * kSkew + bias + kAttnWaves * p.buckets) * sizeof(float) +
+                                (p.dbias ? bias * sizeof(int16_t) : 0);
+            const int done = launch_attention(ctx, attn_dq_kernel<T, DH>, slots * p.heads, rows, s, "attn_dq", p);
+            if (done != FS_OK) return done;
+            const size_t keys = 2 * B * sizeof(tile<T, DH>) + (8 * kTile + 2 * kAttnWaves) * sizeof(float) +
+                                strip<16 * kAttnWaves * KT + kTile>::entries(p.distances, causal) * sizeof(float);
+            return launch_attention(ctx, attn_dkv_kernel<T, DH, KT>, attn_slots(p.n_kv, p.batch, KT == 1 ? 6 : 7) * (p.heads / p.group), keys,
+                                    s, "attn_dkv", p);
+        });
+        if (rc != FS_OK) return rc;
+    }
+    if (!p.dbias) return FS_OK;
+    const int columns = p.heads * p.buckets;
+    if (p.batch > 0) {
+        attn_bias_cut_kernel<<<dim3((unsigned)ceil_div(columns, 64), kBiasCuts), 256, 0, s>>>(p.bias_part, slots, columns, cut);
+        FS_LAUNCH_CHECK(ctx, "attn_bias_cut");
+    }
+    attn_bias_sum_kernel<<<(unsigned)ceil_div(columns, 256), 256, 0, s>>>(cut, p.heads, p.buckets, p.batch > 0 ? kBiasCuts : 0, p.dbias);
+    FS_LAUNCH_CHECK(ctx, "attn_bias_sum");
+    return FS_OK;
+}
+
+}  // namespace fs

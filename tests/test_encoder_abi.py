@@ -26,7 +26,7 @@ def error(blank):
     return fs.load_library().fs_last_error(ctypes.addressof(blank)).decode()
 
 
-@pytest.mark.parametrize("record", ["fs_block_args"])
+@pytest.mark.parametrize("record", ["fs_block_args", "fs_attention_args"])
 def test_records_match_a_c_compiler(tmp_path, record):
     mirror = getattr(fs, record)
     fields = [f[0] for f in mirror._fields_]
@@ -109,6 +109,60 @@ def test_rows8_refuses(blank, rows, stride, dt, n, dim, codes, exps):
     assert "unpack8" in error(blank)
 
 
+def heads(**changes):
+    rec = fs.fs_attention_args(q_stride=128, k_stride=64, v_stride=64, n_q=10, n_kv=20, batch=3, heads=4, kv_heads=2, head_dim=32,
+                               dt=fs.FS_BF16, causal=1, max_q=0, scale=0.2, num_buckets=8, num_distances=30, dq_stride=128, dk_stride=64,
+                               dv_stride=64, work_bytes=1 << 30)
+    for name in ("q", "k", "v", "q_offsets", "kv_offsets", "kv_lengths", "bias", "bucket_of", "out", "out_f32", "lse", "dout", "dq",
+                 "dk", "dv", "dbias", "work"):
+        setattr(rec, name, P)
+    for k, v in changes.items():
+        setattr(rec, k, v)
+    return rec
+
+
+ATTENTION = [dict(n_q=-1), dict(n_kv=-1), dict(batch=-1), dict(batch=0), dict(max_q=-1), dict(heads=0), dict(kv_heads=0), dict(heads=3),
+             dict(heads=-4, kv_heads=-2), dict(heads=2048, kv_heads=1024, q_stride=1 << 20, k_stride=1 << 20, v_stride=1 << 20),
+             dict(head_dim=0), dict(head_dim=36, q_stride=160), dict(head_dim=136, q_stride=1 << 12, k_stride=1 << 12, v_stride=1 << 12),
+             dict(dt=2), dict(scale=float("nan")), dict(scale=float("inf")), dict(causal=2), dict(bucket_of=None), dict(num_buckets=0),
+             dict(num_buckets=1025), dict(num_distances=0), dict(num_distances=4097), dict(n_kv=1 << 31), dict(batch=1 << 31),
+             dict(n_q=1 << 62), dict(q_offsets=None), dict(kv_offsets=None), dict(q_stride=120), dict(k_stride=60), dict(v_stride=-64),
+             dict(q_stride=132), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q=P + 8), dict(k=P + 2), dict(v=P + 4),
+             dict(out=P + 8), dict(out_f32=P + 4)]
+
+
+@pytest.mark.parametrize("changes", ATTENTION + [dict(max_q=1, work=None), dict(max_q=1, work_bytes=8), dict(max_q=1, work=P + 4)])
+def test_jagged_attention_refuses(blank, changes):
+    refused(fs.load_library().fs_jagged_attention(ctypes.addressof(blank), ctypes.byref(heads(**changes)), None))
+    assert "jagged attention" in error(blank)
+
+
+@pytest.mark.parametrize("changes", ATTENTION + [dict(dout=None), dict(dq=None), dict(lse=None), dict(dk=None), dict(dv=None),
+                                                 dict(dq_stride=120), dict(dk_stride=66), dict(dv_stride=0), dict(dout=P + 8),
+                                                 dict(dq=P + 8), dict(dk=P + 8), dict(dv=P + 8), dict(work=None), dict(work_bytes=8),
+                                                 dict(work=P + 8)])
+def test_jagged_attention_backward_refuses(blank, changes):
+    refused(fs.load_library().fs_jagged_attention_backward(ctypes.addressof(blank), ctypes.byref(heads(**changes)), None))
+    assert "jagged attention" in error(blank)
+
+
+def test_attention_without_records_and_rows(blank):
+    lib, ctx = fs.load_library(), ctypes.addressof(blank)
+    for call in (lib.fs_jagged_attention, lib.fs_jagged_attention_backward):
+        refused(call(None, ctypes.byref(heads()), None))
+        refused(call(ctx, None, None))
+    assert lib.fs_jagged_attention(ctx, ctypes.byref(heads(n_q=0)), None) == fs.FS_OK
+    assert lib.fs_jagged_attention(ctx, ctypes.byref(heads(n_q=0, n_kv=0, batch=0)), None) == fs.FS_OK
+    for size in (lib.fs_jagged_attention_work_bytes, lib.fs_jagged_attention_backward_work_bytes):
+        assert size(None) == 0 and size(ctypes.byref(heads(heads=3))) == 0
+    assert lib.fs_jagged_attention_work_bytes(ctypes.byref(heads())) == 0
+    assert lib.fs_jagged_attention_work_bytes(ctypes.byref(heads(max_q=9))) == 0       # 18 columns: the other form
+    few = lib.fs_jagged_attention_work_bytes(ctypes.byref(heads(max_q=2)))
+    assert few > 0 and lib.fs_jagged_attention_work_bytes(ctypes.byref(heads(max_q=2, n_kv=20_000))) > few
+    assert lib.fs_jagged_attention_backward_work_bytes(ctypes.byref(heads(dbias=None))) < \
+        lib.fs_jagged_attention_backward_work_bytes(ctypes.byref(heads()))
+
+
 class Stub:
     """A context for the checks of the binding, which come before the library is called."""
     device, handle = 0, None
@@ -116,6 +170,22 @@ class Stub:
 
     def check(self, rc, where):
         raise AssertionError("reached the library")
+
+
+@pytest.mark.parametrize("changes", [
+    dict(),                                                                                   # not on the GPU
+    dict(k=torch.zeros(7, 2, 8)), dict(v=torch.zeros(7, 2, 16).transpose(0, 1)), dict(q=torch.zeros(7, 16)),
+    dict(q=torch.zeros(7, 2, 16).half()), dict(k=torch.zeros(7, 2, 16).bfloat16()), dict(q=torch.zeros(7, 2, 32)[:, :, ::2]),
+    dict(q=torch.zeros(7, 4, 16)[:, ::2]), dict(q_offsets=torch.zeros(4, dtype=torch.int32)),
+    dict(kv_offsets=torch.zeros(5, dtype=torch.int64)), dict(kv_lengths=torch.zeros(4, dtype=torch.int64)),
+    dict(bias=torch.zeros(4, 3)), dict(bias=torch.zeros(4, 2).double()), dict(bucket_of=torch.zeros(4, dtype=torch.int64)),
+    dict(causal=False, bucket_of=torch.zeros(4, dtype=torch.int32)), dict(out={"out": torch.zeros(7, 2, 8)}),
+    dict(out={"lse": torch.zeros(7, 2)})])
+def test_binding_refuses_attention(changes):
+    args = dict(q=torch.zeros(7, 2, 16), k=torch.zeros(7, 2, 16), v=torch.zeros(7, 2, 16), q_offsets=torch.zeros(4, dtype=torch.int64),
+                kv_offsets=torch.zeros(4, dtype=torch.int64), bias=torch.zeros(4, 2), bucket_of=torch.zeros(4, dtype=torch.int32))
+    with pytest.raises((ValueError, TypeError)):
+        fs.fs_jagged_attention(Stub(), **{**args, **changes})
 
 
 @pytest.mark.parametrize("call", [
