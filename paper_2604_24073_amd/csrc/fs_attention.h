@@ -267,24 +267,43 @@ struct user {
     int first;                               // position of its first query row among its keys: nk - nq, may be negative
 };
 
-// Slots: tiles of 2^shift rows of one user, numbered so that a user's begin at offsets[b] / 2^shift + b, which leaves room for
-// one that is cut off at each end and needs nobody to add up the tiles before.  Finds the user of a slot (a 64-ary search by
-// the whole wavefront) and which of its tiles the slot is; false where there is none.  Boundaries that do not fit are flagged
-// and their user left out; every access stays inside the rows whatever the offsets hold.
-__device__ __forceinline__ bool find_user(const attn_params &p, const int64_t *__restrict__ offsets, int64_t slot, int shift, user &u,
-                                          int &index) {
+// The last of the users [0, count) whose offsets[b] / 2^shift + step b is at most `value`, 0 if there is none; a 64-ary search by
+// the whole wavefront, which stays among the users whatever the offsets hold.  In 32 bits: for 64-bit bounds, which are the same
+// in every lane, this compiler has made two selections of one comparison's outcome.
+__device__ __forceinline__ int last_user(const int64_t *__restrict__ offsets, int count, int shift, int per_user, int64_t value) {
     const int lane = threadIdx.x & 63;
-    int64_t lo = 0, hi = p.batch - 1;        // user lo begins at or before the slot (or there is no such user)
+    int lo = 0, hi = count - 1;
     while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64;
-        const int64_t probe = lo + (lane + 1) * step;
-        const bool le = probe <= hi && (offsets[probe] >> shift) + probe <= slot;
+        const int step = (int)((unsigned)(hi - lo + 63) / 64u), left = hi - lo, ahead = left / step;      // probes that exist
+        bool le = false;
+        if (lane < ahead) {
+            const int probe = lo + (lane + 1) * step;
+            le = (offsets[probe] >> shift) + (int64_t)per_user * probe <= value;
+        }
         const int cnt = __popcll(__ballot(le));
-        const int64_t nhi = lo + (cnt + 1) * step - 1;
-        lo += cnt * step;
-        hi = nhi < hi ? nhi : hi;
-        hi = hi < lo ? lo : hi;
+        const int span = min((cnt + 1) * step - 1, left);
+        hi = lo + span;
+        lo = lo + cnt * step;
     }
+    return lo;
+}
+
+// The rows in use of a user with so many rows: lengths[b], brought into [0, room].
+__device__ __forceinline__ int rows_in_use(const int64_t *__restrict__ lengths, int64_t b, int room) {
+    if (!lengths) return room;
+    const int64_t used = lengths[b];
+    const int high = (int)(used >> 32), low = (int)used;
+    const int some = high > 0 ? room : low < 0 ? room : min(low, room);
+    return high < 0 ? 0 : some;
+}
+
+// Slots: tiles of 2^shift rows of one user, numbered so that a user's begin at offsets[b] / 2^shift + b, which leaves room for
+// one that is cut off at each end and needs nobody to add up the tiles before.  Finds the user of a slot and which of its tiles
+// the slot is; false where there is none.  Boundaries that do not fit leave their user out; every access stays inside the rows
+// whatever the offsets hold.
+__device__ __forceinline__ bool find_user(const attn_params &p, const int64_t *__restrict__ offsets, int slot, int shift, user &u,
+                                          int &index) {
+    const int lo = last_user(offsets, (int)p.batch, shift, 1, slot);
     u.b = lo;
     const int64_t qa = p.q_offsets[lo], qb = p.q_offsets[lo + 1], ka = p.kv_offsets[lo], kb = p.kv_offsets[lo + 1];
     if (qa < 0 || qb < qa || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv || qb - qa > 0x3fffffff || kb - ka > 0x3fffffff)
@@ -292,11 +311,8 @@ __device__ __forceinline__ bool find_user(const attn_params &p, const int64_t *_
     u.q0 = qa;
     u.k0 = ka;
     u.nq = (int)(qb - qa);
-    u.nk = u.room = (int)(kb - ka);
-    if (p.kv_lengths) {
-        const int64_t used = p.kv_lengths[lo];
-        u.nk = used < 0 ? 0 : used < u.nk ? (int)used : u.nk;
-    }
+    u.room = (int)(kb - ka);
+    u.nk = rows_in_use(p.kv_lengths, lo, u.room);
     u.first = u.nk - u.nq;
     const int64_t k = slot - ((offsets[lo] >> shift) + lo);
     index = (int)k;

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
 
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
     const int head = blockIdx.x % p.heads;
-    const int64_t slot = blockIdx.x / p.heads;
+    const int slot = (int)(blockIdx.x / p.heads);
     if (head == 0) check_layout(p, slot);
     user u;
     int index;
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_split_kernel(attn_params p)
     float *bias_lds = reinterpret_cast<float *>(lds + kAttnWaves * sizeof(tile<T, DH>));
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
     const int kv_heads = p.heads / p.group, kvh = blockIdx.x % kv_heads;
-    const int64_t slot = blockIdx.x / kv_heads;
+    const int slot = (int)(blockIdx.x / kv_heads);
     if (kvh == 0) check_layout(p, slot);
     user u;
     int index;
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_split_kernel(attn_params p)
                 if (p.out_f32) store4(p.out_f32 + at, o);
             }
         } else {
-            const int64_t at = (slot * kv_heads + kvh) * (max_q * p.group) + c;
+            const int64_t at = ((int64_t)slot * kv_heads + kvh) * (max_q * p.group) + c;
             if (col == 0) {
                 p.split_ml[2 * at] = top;
                 p.split_ml[2 * at + 1] = sum;
@@ -434,32 +434,18 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(attn_params p) 
     const int head = (int)(item % p.heads);
     const int64_t at_row = item / p.heads;
     if (at_row >= p.n_q) return;
-    user u;
-    int row;
     // users without query rows begin where their successor does; the last one at or before a row is the row's
-    int64_t lo = 0, hi = p.batch - 1;
-    while (lo < hi) {
-        const int64_t step = (hi - lo + 63) / 64, probe = lo + (lane + 1) * step;
-        const int cnt = __popcll(__ballot(probe <= hi && p.q_offsets[probe] <= at_row));
-        const int64_t nhi = lo + (cnt + 1) * step - 1;
-        lo += cnt * step;
-        hi = nhi < hi ? nhi : hi;
-        hi = hi < lo ? lo : hi;
-    }
-    const int64_t qa = p.q_offsets[lo], qb = p.q_offsets[lo + 1], ka = p.kv_offsets[lo], kb = p.kv_offsets[lo + 1];
+    const int b = last_user(p.q_offsets, (int)p.batch, 0, 0, at_row);
+    const int64_t qa = p.q_offsets[b], qb = p.q_offsets[b + 1], ka = p.kv_offsets[b], kb = p.kv_offsets[b + 1];
     if (qa < 0 || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv || at_row < qa || at_row >= qb || qb - qa > max_q ||
         kb - ka > 0x3fffffff)
         return;
-    u.nk = (int)(kb - ka);
-    if (p.kv_lengths) {
-        const int64_t used = p.kv_lengths[lo];
-        u.nk = used < 0 ? 0 : used < u.nk ? (int)used : u.nk;
-    }
+    const int nk = rows_in_use(p.kv_lengths, b, (int)(kb - ka));
     const int chunk = 1 << shift;
-    if (u.nk <= chunk) return;                          // written by the workgroup that had them all
-    row = (int)(at_row - qa);
-    const int kv_heads = p.heads / p.group, kvh = head / p.group, chunks = (u.nk + chunk - 1) >> shift;
-    const int64_t slot0 = (ka >> shift) + lo;
+    if (nk <= chunk) return;                            // written by the workgroup that had them all
+    const int row = (int)(at_row - qa);
+    const int kv_heads = p.heads / p.group, kvh = head / p.group, chunks = (nk + chunk - 1) >> shift;
+    const int64_t slot0 = (ka >> shift) + b;
     const int64_t first = (slot0 * kv_heads + kvh) * (max_q * p.group) + row * p.group + head % p.group;
     const int64_t apart = (int64_t)kv_heads * max_q * p.group;
     float top = neg_inf();

@@ -91,11 +91,11 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dq_kernel(attn_params p) {
 
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
     const int head = blockIdx.x % p.heads;
-    const int64_t slot = blockIdx.x / p.heads;
+    const int slot = (int)(blockIdx.x / p.heads);
     if (head == 0) check_layout(p, slot);
     user u;
     int index;
-    float *part = p.dbias ? p.bias_part + (slot * p.heads + head) * p.buckets : nullptr;
+    float *part = p.dbias ? p.bias_part + ((int64_t)slot * p.heads + head) * p.buckets : nullptr;
     if (!find_user(p, p.q_offsets, slot, kShift, u, index) || (int64_t)index * kRows >= u.nq) {
         if (part)
             for (int b = threadIdx.x; b < p.buckets; b += kAttnThreads) part[b] = 0.f;
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_kernel(attn_params p) {
     const int kv_heads = p.heads / p.group, kvh = blockIdx.x % kv_heads;
     user u;
     int index;
-    if (!find_user(p, p.kv_offsets, blockIdx.x / kv_heads, kShift, u, index) || (int64_t)index * kKeys >= u.room) return;
+    if (!find_user(p, p.kv_offsets, (int)(blockIdx.x / kv_heads), kShift, u, index) || (int64_t)index * kKeys >= u.room) return;
     const int key_first = index * kKeys;
     const int wkey = key_first + 16 * KT * w;
     // query rows at or behind the first key; every tile of 64 of them, for every head that shares the keys

@@ -439,3 +439,13 @@ def test_captured_and_replayed(ctx):
             want = call()
             for name in want:
                 assert torch.equal(res[name], want[name]), (turn, name)
+
+
+@pytest.mark.parametrize("users", [64, 65, 66, 129, 200, 256, 1000, 4097])
+def test_many_users(ctx, users):
+    """Every user is found, the last ones among them, by tiles of rows, of keys and by row."""
+    lens = [(7 * u) % 5 for u in range(users)]
+    Case(lens, heads=1, kv_heads=1, width=8, dtype=BF16).check(ctx)
+    c = Case([1] * users, [260 + u % 3 for u in range(users)], heads=1, kv_heads=1, width=8, dtype=BF16, buckets=0)
+    got = c.forward(ctx, max_q=1, out={"out": torch.full_like(c.q, float("nan")).cuda()})["out"]
+    assert_bounded(got, *c.want(False)["out"], "few")
