@@ -15,7 +15,11 @@ namespace {
 // query rows of a workgroup whose wavefronts have QT times sixteen
 constexpr int fwd_rows(int qt) { return 16 * kAttnWaves * qt; }
 
-template <typename T, int DH, int QT>
+// EXACT, of bf16 rows whose unrounded out is wanted: P goes into its product as two terms.  The bias's gradient adds up
+// differences of dO V^T and D = dO . out that cancel over a row, and an out made of rounded P leaves their errors in it (a
+// batch of 297 k rows: off by 1e-3 of itself, with both terms by 2e-6).  The matrix cores have the time: the softmax's share of
+// the vector units decides (DH = 32, the same batch: 940 us with, 900 without).
+template <typename T, int DH, int QT, bool EXACT>
 __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params p) {
     constexpr int kRows = fwd_rows(QT), kShift = QT == 1 ? 6 : 7, kPad = kRows + kTile;
     constexpr int KC = DH / 32, MT = DH / 16;
@@ -161,15 +165,21 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                piece<T> pf[QT];
+                piece<T> pf[QT], rest[QT];
 #pragma unroll
-                for (int t = 0; t < QT; ++t) as_operand(pf[t], s[t][2 * c], s[t][2 * c + 1]);
+                for (int t = 0; t < QT; ++t) {
+                    if constexpr (EXACT) as_operands(pf[t], rest[t], s[t][2 * c], s[t][2 * c + 1]);
+                    else as_operand(pf[t], s[t][2 * c], s[t][2 * c + 1]);
+                }
 #pragma unroll
                 for (int d = 0; d < MT; ++d) {
                     piece<T> a;
                     V.cols(a, 32 * c, 16 * d);
 #pragma unroll
-                    for (int t = 0; t < QT; ++t) mma(acc[t][d], a, pf[t]);
+                    for (int t = 0; t < QT; ++t) {
+                        mma(acc[t][d], a, pf[t]);
+                        if constexpr (EXACT) mma(acc[t][d], a, rest[t]);
+                    }
                 }
             }
             settle();
@@ -616,14 +626,20 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
             if (done != FS_OK || a.n_kv <= 1ll << p.split_shift) return done;     // nobody has several chunks
             return launch_attention(ctx, attn_join_kernel<T, DH>, ceil_div(a.n_q * a.heads, kAttnWaves), 0, s, "attn_join", p);
         }
-        const auto run = [&](auto qt) {
+        const auto run = [&](auto qt, auto exact) {
             constexpr int QT = qt();
             const size_t lds = 2 * tile_buffers<T, DH> * sizeof(tile<T, DH>) + 2 * kAttnWaves * sizeof(uint32_t) +
                                strip<fwd_rows(QT) + kTile>::entries(p.distances, a.causal != 0) * sizeof(float);
-            return launch_attention(ctx, attn_forward_kernel<T, DH, QT>, attn_slots(a.n_q, a.batch, QT == 1 ? 6 : 7) * a.heads, lds, s,
+            return launch_attention(ctx, attn_forward_kernel<T, DH, QT, exact()>, attn_slots(a.n_q, a.batch, QT == 1 ? 6 : 7) * a.heads, lds, s,
                                     "attn_forward", p);
         };
-        return forward_qt(a) == 2 ? run(std::integral_constant<int, 2>()) : run(std::integral_constant<int, 1>());
+        const auto rows = [&](auto exact) {
+            return forward_qt(a) == 2 ? run(std::integral_constant<int, 2>(), exact) : run(std::integral_constant<int, 1>(), exact);
+        };
+        if constexpr (sizeof(T) == 2) {
+            if (p.out_f32) return rows(std::true_type());
+        }
+        return rows(std::false_type());
     });
 }
 
