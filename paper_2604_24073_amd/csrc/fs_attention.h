@@ -275,6 +275,9 @@ struct attn_params {
     int *flags;
 };
 
+// the wavefront's number in its workgroup, known to be the same in every lane
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
 struct user {
     int64_t q0, k0;                          // first row of its queries, of its keys
     int64_t b;
@@ -389,6 +392,11 @@ struct strip {
     }
 };
 
+// Wavefronts of a SIMD that a kernel is compiled for.  With two or more of them asked for, all of a wavefront's registers can be
+// named by every instruction, and the accumulators stay where the vector units can read them.
+template <typename T, int DH>
+constexpr int attn_waves = sizeof(T) * DH <= 128 ? 2 : 1;
+
 // ---- host side --------------------------------------------------------------------------------------------------------------
 constexpr int kMaxLds = 160 * 1024;
 constexpr int kFreeLds = 64 * 1024;           // what a kernel may ask for without saying so beforehand
@@ -418,6 +426,6 @@ int by_head(int dt, int width, F &&f) {
 inline int64_t attn_slots(int64_t rows, int64_t batch, int shift) { return (rows >> shift) + batch; }
 
 int launch_attention_backward(fs_ctx *ctx, const attn_params &p, int dt, void *work, hipStream_t s);
-size_t attention_backward_work(const attn_params &p);
+size_t attention_backward_work(const attn_params &p, int dt);
 
 }  // namespace fs

@@ -20,7 +20,7 @@ constexpr int fwd_rows(int qt) { return 16 * kAttnWaves * qt; }
 // batch of 297 k rows: off by 1e-3 of itself, with both terms by 2e-6).  The matrix cores have the time: the softmax's share of
 // the vector units decides (DH = 32, the same batch: 940 us with, 900 without).
 template <typename T, int DH, int QT, bool EXACT>
-__global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params p) {
+__global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forward_kernel(attn_params p) {
     constexpr int kRows = fwd_rows(QT), kShift = QT == 1 ? 6 : 7, kPad = kRows + kTile;
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
     uint32_t *odd = reinterpret_cast<uint32_t *>(vt + kBufs);        // [2][wavefronts]: the tile had values that are no numbers
     float *bias_lds = reinterpret_cast<float *>(odd + 2 * kAttnWaves);
 
-    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int head = blockIdx.x % p.heads;
     const int slot = (int)(blockIdx.x / p.heads);
     if (head == 0) check_layout(p, slot);
@@ -62,7 +62,8 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
     const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last, nullptr);
     const float scale2 = p.scale * kLog2e;
 
-    f32x4 acc[QT][MT] = {};
+    // the product with P's second term has a sum of its own: an infinity among the values meets a zero or a negative rest there
+    f32x4 acc[QT][MT] = {}, acc_rest[EXACT ? QT : 1][MT] = {};
     float m[QT], l[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -114,7 +115,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[t][k][r] = s[t][k][r] * scale2 + b;
             } else {
-                const float *b = bias.at + bias.zero + (wpos + j - key0 - 4 * g) - 51;
+                const float *b = bias.at + bias.zero + nearest + (j - 4 * g) + 12;
 #pragma unroll
                 for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -152,7 +153,10 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
 #pragma unroll
                     for (int c = 0; c < MT; ++c)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[t][c][r] *= shrink;
+                        for (int r = 0; r < 4; ++r) {
+                            acc[t][c][r] *= shrink;
+                            if constexpr (EXACT) acc_rest[t][c][r] *= shrink;
+                        }
                 }
                 const float base = m[t] == neg_inf() ? 0.f : m[t];
 #pragma unroll
@@ -178,7 +182,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
                         mma(acc[t][d], a, pf[t]);
-                        if constexpr (EXACT) mma(acc[t][d], a, rest[t]);
+                        if constexpr (EXACT) mma(acc_rest[t][d], a, rest[t]);
                     }
                 }
             }
@@ -224,7 +228,11 @@ __global__ __launch_bounds__(kAttnThreads) void attn_forward_kernel(attn_params 
             const int col = 16 * c + 4 * g;
             f32x4 o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = acc[t][c][r] * inv;
+            for (int r = 0; r < 4; ++r) {
+                float x = acc[t][c][r];
+                if constexpr (EXACT) x += fabsf(x) < __builtin_inff() ? acc_rest[t][c][r] : 0.f;
+                o[r] = x * inv;
+            }
             if (col < p.width) {
                 store4(static_cast<T *>(p.out) + at + col, o);
                 if (p.out_f32) store4(p.out_f32 + at + col, o);
@@ -242,14 +250,14 @@ constexpr int kSplitCols = 16;
 constexpr int kSplitStep = kAttnWaves * kTile;        // keys of a workgroup at a time
 
 template <typename T, int DH>
-__global__ __launch_bounds__(kAttnThreads) void attn_split_kernel(attn_params p) {
+__global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_split_kernel(attn_params p) {
     const int shift = p.split_shift, max_q = p.max_q;
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
     tile<T, DH> *vt = reinterpret_cast<tile<T, DH> *>(lds);                                   // [wavefronts]
     float *merge = reinterpret_cast<float *>(lds);                                            // the same memory, afterwards
     float *bias_lds = reinterpret_cast<float *>(lds + kAttnWaves * sizeof(tile<T, DH>));
-    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int kv_heads = p.heads / p.group, kvh = blockIdx.x % kv_heads;
     const int slot = (int)(blockIdx.x / kv_heads);
     if (kvh == 0) check_layout(p, slot);
@@ -440,7 +448,7 @@ template <typename T, int DH>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(attn_params p) {
     const int shift = p.split_shift, max_q = p.max_q;
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * kAttnWaves + (threadIdx.x >> 6);
+    const int64_t item = (int64_t)blockIdx.x * kAttnWaves + wave_id();
     const int head = (int)(item % p.heads);
     const int64_t at_row = item / p.heads;
     if (at_row >= p.n_q) return;
@@ -645,7 +653,7 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
 
 size_t fs_jagged_attention_backward_work_bytes(const fs_attention_args *args) {
     if (!args || attn_check(nullptr, *args) != FS_OK) return 0;
-    return attention_backward_work(params_of(nullptr, *args));
+    return attention_backward_work(params_of(nullptr, *args), args->dt);
 }
 
 int fs_jagged_attention_backward(fs_ctx *ctx, const fs_attention_args *args, fs_stream stream) {
@@ -665,7 +673,7 @@ int fs_jagged_attention_backward(fs_ctx *ctx, const fs_attention_args *args, fs_
     FS_NEED(aligned16(a.dout) && aligned16(a.dq) && aligned16(a.dk) && aligned16(a.dv),
             "jagged attention backward: pointer not 16-byte aligned");
     attn_params p = params_of(ctx, a);
-    const size_t need = attention_backward_work(p);
+    const size_t need = attention_backward_work(p, a.dt);
     FS_NEED(need == 0 || (a.work && aligned16(a.work) && a.work_bytes >= need),
             "jagged attention backward: work is null, not 16-byte aligned or too small");
     device_scope on(ctx->device);

@@ -38,23 +38,48 @@ struct bucket_sums {
         }
         run += share;
     }
-    // every lane's value of a bucket of its own: bucket after bucket
+    // Every lane's value of a bucket of its own, the lanes' distances ascending.  Runs of a bucket are added up by a scan that
+    // starts anew where the bucket changes, and each run's last lane has its sum; buckets that come back after another one
+    // (no table of distances needs them to) are taken one after the other.
     __device__ __forceinline__ void each(int bucket, float value) {
-        uint64_t left = __ballot(bucket >= 0);
-        while (left) {
-            const int b = __builtin_amdgcn_readlane(bucket, __ffsll((unsigned long long)left) - 1);
-            const bool mine = bucket == b;
-            add(b, wave_sum(mine ? value : 0.f));
-            left &= ~__ballot(mine);
+        const int lane = threadIdx.x & 63;
+        const int before = __builtin_amdgcn_update_dpp(bucket, bucket, 0x138, 0xf, 0xf, false);        // wave_shr:1
+        const uint64_t heads = __ballot(bucket != before) | 1;
+        if (__ballot(bucket > before) && __ballot(bucket < before)) {
+            uint64_t left = __ballot(bucket >= 0);
+            while (left) {
+                const int b = __builtin_amdgcn_readlane(bucket, __ffsll((unsigned long long)left) - 1);
+                const bool mine = bucket == b;
+                add(b, wave_sum(mine ? value : 0.f));
+                left &= ~__ballot(mine);
+            }
+            return;
         }
+        const int start = 63 - __clzll((long long)(heads & (~0ull >> (63 - lane))));
+        const int in_row = lane & 15;
+        float x = value;
+#pragma unroll
+        for (int d = 1; d < 16; d <<= 1) {
+            const float y = __uint_as_float(__builtin_amdgcn_ds_bpermute(4 * (lane - d), (int)__float_as_uint(x)));
+            x += in_row >= d && lane - d >= start ? y : 0.f;
+        }
+        {
+            const float y = __uint_as_float(__builtin_amdgcn_ds_bpermute(4 * ((lane & 32) + 15), (int)__float_as_uint(x)));
+            x += (lane & 16) && (lane & 32) + 15 >= start ? y : 0.f;
+            const float z = __uint_as_float(__builtin_amdgcn_ds_bpermute(4 * 31, (int)__float_as_uint(x)));
+            x += (lane & 32) && 31 >= start ? z : 0.f;
+        }
+        const bool last = lane == 63 || ((heads >> 1) >> lane & 1);
+        if (last && bucket >= 0) bins[bucket] += x;
     }
 };
 
 // A wavefront's 16 query rows x 64 keys, summed along its diagonals: value (q, key) belongs to distance q - key + 63 of the
 // 79.  Each value is written where its distance's row has column q; a row then has at most 16, and rows d and d + 64 share
 // them: row d has columns up to d, row d + 64 those behind.
+constexpr int kSpan = kTile + 15;
 constexpr int kSkewLd = 17;
-constexpr int kSkew = (kTile + 15) * kSkewLd;
+constexpr int kSkew = kSpan * kSkewLd;
 __device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], float &near, float &far) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
 #pragma unroll
@@ -68,28 +93,64 @@ __device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], 
 #pragma unroll
     for (int q = 0; q < 16; ++q) {
         const float x = row[q + (q > cut ? 64 * kSkewLd : 0)];
-        if (q <= cut) near += x;
-        else far += x;
+        near += q <= cut ? x : 0.f;
+        far += q <= cut ? 0.f : x;
     }
     wave_lds_order();
 }
 
+// The 16 x 64 values s of a wavefront, whose distances are 79 that ascend in `buckets`, added to the sums of their buckets.
+// Tables of distances have few buckets in 79 distances but near zero: one bucket takes every lane's sum as it is, two
+// are told apart by comparing distances, and only more are brought into the order of the distances.  Further distances come
+// first: the tiles go from far to near, and a bucket's lanes are added up when the next bucket begins.
+__device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, const f32x4 (&s)[4], const int16_t *buckets) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+    const int b0 = buckets[lane], b1 = buckets[lane < 15 ? 64 + lane : 78];
+    const int last0 = __builtin_amdgcn_readlane(b0, 63), before0 = __builtin_amdgcn_update_dpp(b0, b0, 0x138, 0xf, 0xf, false);
+    int before1 = __builtin_amdgcn_update_dpp(b1, b1, 0x138, 0xf, 0xf, false);
+    before1 = lane == 0 ? last0 : before1;
+    uint64_t h0 = __ballot(b0 != before0), h1 = __ballot(b1 != before1);          // where a bucket begins
+    const int changes = __popcll(h0) + __popcll(h1);
+    if (changes > 1) {
+        float near, far;
+        diagonal_sums(skew, s, near, far);
+        sums.each(b0, near);
+        sums.each(b1, lane < 15 ? far : 0.f);
+        return;
+    }
+    // the distances from `at` on have another bucket than those before (none of them where nothing changes)
+    const int at = h0 ? 63 - __clzll((long long)h0) : h1 ? 127 - __clzll((long long)h1) : kSpan;
+    const int mine = j + 63 - 4 * g;                       // element r of s[k] has distance mine - 16 k - r
+    float near = 0.f, far = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const bool beyond = mine >= at + 16 * k + r;
+            far += beyond ? s[k][r] : 0.f;
+            near += beyond ? 0.f : s[k][r];
+        }
+    if (changes) sums.one(__builtin_amdgcn_readlane(b1, 14), far);
+    sums.one(__builtin_amdgcn_readfirstlane(b0), near);
+}
+
 // ---- query rows ---------------------------------------------------------------------------------------------------------------
-template <typename T, int DH>
-__global__ __launch_bounds__(kAttnThreads) void attn_dq_kernel(attn_params p) {
-    constexpr int kRows = 16 * kAttnWaves, kShift = 6, kPad = kRows + kTile;
+// QT: sixteens of query rows of a wavefront
+template <typename T, int DH, int QT>
+__global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_kernel(attn_params p) {
+    constexpr int kRows = 16 * kAttnWaves * QT, kShift = QT == 1 ? 6 : 7, kPad = kRows + kTile;
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
     constexpr int kBufs = tile_buffers<T, DH>;
     tile<T, DH> *kt = reinterpret_cast<tile<T, DH> *>(lds), *vt = kt + kBufs;
-    float *mark = reinterpret_cast<float *>(vt + kBufs);                              // [2][kTile]
+    float *mark = reinterpret_cast<float *>(vt + kBufs);                          // [2][kTile]
     float *skew = mark + 2 * kTile;                                               // [wavefronts][kSkew]
     float *bias_lds = skew + kAttnWaves * kSkew;
     const int entries = strip<kPad>::entries(p.distances, p.causal != 0);
     float *bins = bias_lds + entries;                                             // [wavefronts][buckets]
     int16_t *bucket_lds = reinterpret_cast<int16_t *>(bins + kAttnWaves * p.buckets);
 
-    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int head = blockIdx.x % p.heads;
     const int slot = (int)(blockIdx.x / p.heads);
     if (head == 0) check_layout(p, slot);
@@ -113,32 +174,38 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dq_kernel(attn_params p) {
     kr.load(kbase, p.k_stride, tiles ? u.nk : 0, p.width);
     vr.load(vbase, p.v_stride, tiles ? u.nk : 0, p.width);
 
-    const int wrow = row0 + 16 * w, wpos = u.first + wrow, row = wrow + j;
-    const bool live = row < u.nq;
-    piece<T> qf[KC], of[KC];
+    const int wrow = row0 + 16 * QT * w, wpos = u.first + wrow;
+    piece<T> qf[QT][KC], of[QT][KC];
+    float delta[QT], lse2[QT];
     const int64_t orow = p.heads * (int64_t)p.width;                              // out and dout are packed
     const int64_t obase = u.q0 * orow + head * p.width;
-    float delta = 0.f;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) {
-        global_rows(qf[c], static_cast<const T *>(p.q) + u.q0 * p.q_stride + head * p.width, p.q_stride, row, live, 32 * c, p.width);
-        global_rows(of[c], static_cast<const T *>(p.dout) + obase, orow, row, live, 32 * c, p.width);
-        const int col = 32 * c + 8 * g, left = live ? p.width - col : 0;
-        const int64_t at = obase + row * orow + col;
-        float o[8], d[8];
-        if (p.out_f32) load8(p.out_f32 + at, left, o);
-        else load8(static_cast<const T *>(p.out) + at, left, o);
-        load8(static_cast<const T *>(p.dout) + at, left, d);
+    for (int t = 0; t < QT; ++t) {
+        const int row = wrow + 16 * t + j;
+        const bool live = row < u.nq;
+        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) delta += o[i] * d[i];
-    }
-    delta = column_sum(delta);
-    float lse2 = __builtin_inff();                                                // a row that sees nothing: P = 0
-    if (live) {
-        const int64_t at = (int64_t)head * p.n_q + u.q0 + row;
-        const float x = p.lse[at];
-        if (x != neg_inf()) lse2 = x * kLog2e;
-        if (g == 0) p.delta[at] = delta;
+        for (int c = 0; c < KC; ++c) {
+            global_rows(qf[t][c], static_cast<const T *>(p.q) + u.q0 * p.q_stride + head * p.width, p.q_stride, row, live, 32 * c,
+                        p.width);
+            global_rows(of[t][c], static_cast<const T *>(p.dout) + obase, orow, row, live, 32 * c, p.width);
+            const int col = 32 * c + 8 * g, left = live ? p.width - col : 0;
+            const int64_t at = obase + row * orow + col;
+            float o[8], d[8];
+            if (p.out_f32) load8(p.out_f32 + at, left, o);
+            else load8(static_cast<const T *>(p.out) + at, left, o);
+            load8(static_cast<const T *>(p.dout) + at, left, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += o[i] * d[i];
+        }
+        delta[t] = column_sum(sum);
+        lse2[t] = __builtin_inff();                                               // a row that sees nothing: P = 0
+        if (live) {
+            const int64_t at = (int64_t)head * p.n_q + u.q0 + row;
+            const float x = p.lse[at];
+            if (x != neg_inf()) lse2[t] = x * kLog2e;
+            if (g == 0) p.delta[at] = delta[t];
+        }
     }
     strip<kPad> bias;
     bucket_sums sums;
@@ -148,7 +215,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dq_kernel(attn_params p) {
     const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last, part ? bucket_lds : nullptr);
     const float scale2 = p.scale * kLog2e;
 
-    f32x4 acc[MT] = {};
+    f32x4 acc[QT][MT] = {};
     // some rows do not see all keys of the tile, or some of those are none
     const auto edge = [&](int n) { return hides || (n + 1) * kTile > u.nk || (p.causal && (n + 1) * kTile - 1 > pos0); };
     const auto stage = [&](int n) {
@@ -168,88 +235,95 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dq_kernel(attn_params p) {
             vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile, p.width);
         }
         const tile<T, DH> &K = kt[n & (kBufs - 1)], &V = vt[n & (kBufs - 1)];
-        if (wrow < u.nq && !(p.causal && key0 > wpos + 15)) {
-            f32x4 s[4], dp[4];
+        if (wrow < u.nq && !(p.causal && key0 > wpos + 16 * QT - 1)) {
+            f32x4 s[QT][4], dp[QT][4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                s[k] = dp[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < QT; ++t) s[t][k] = dp[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < KC; ++c) {
                     piece<T> a;
                     K.rows(a, 16 * k, 32 * c);
-                    mma(s[k], a, qf[c]);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) mma(s[t][k], a, qf[t][c]);
                     V.rows(a, 16 * k, 32 * c);
-                    mma(dp[k], a, of[c]);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) mma(dp[t][k], a, of[t][c]);
                 }
             }
-            const int nearest = wpos - (key0 + kTile - 1), furthest = wpos + 15 - key0;
+            // element r of s[t][k]: query row wrow + 16 t + j, key key0 + 16 k + 4 g + r
+            const int nearest = wpos - (key0 + kTile - 1), furthest = wpos + 16 * QT - 1 - key0;
             const bool all_far = nearest >= bias.high || furthest <= bias.low;
             const int far_at = bias.zero + (nearest >= bias.high ? bias.high : bias.low);
             const float far = bias.at[far_at];
-            const float *bb = bias.at + bias.zero + (wpos + j - key0 - 4 * g) - 51;
-            const auto score = [&](auto mask) {
-                const int seen = p.causal ? min(wpos + j + 1, u.nk) : u.nk;          // keys that the row sees
+            // of a tile beyond the table, the distances nearest to it have the same bias
+            const int near = min(max(nearest, bias.low - (62 + 16 * QT)), bias.high);
+            const float *bb = bias.at + bias.zero + near + (j - 4 * g) + 12;
+            const auto score = [&](auto mask, auto away) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     f32x4 x;
                     if constexpr (mask()) x = *reinterpret_cast<const f32x4 *>(mark + (n & 1) * kTile + 16 * k + 4 * g);
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float b = all_far ? far : bb[51 - 16 * k - r];
-                        float power = s[k][r] * scale2 + b - lse2, d = dp[k][r] - delta;
-                        if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen ? power + x[r] : neg_inf();
-                        const float e = __builtin_amdgcn_exp2f(power);
-                        if constexpr (mask()) d = e == 0.f ? 0.f : d;
-                        s[k][r] = e * d;
+                    for (int t = 0; t < QT; ++t) {
+                        const int seen = p.causal ? min(wpos + 16 * t + j + 1, u.nk) : u.nk;     // keys that the row sees
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float b = away() ? far : bb[51 + 16 * t - 16 * k - r];
+                            float power = s[t][k][r] * scale2 + (b - lse2[t]), d = dp[t][k][r] - delta[t];
+                            if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen ? power + x[r] : neg_inf();
+                            const float e = __builtin_amdgcn_exp2f(power);
+                            if constexpr (mask()) d = e == 0.f ? 0.f : d;
+                            s[t][k][r] = e * d;
+                        }
                     }
                 }
             };
-            if (edge(n)) score(std::true_type());
-            else score(std::false_type());
+            if (edge(n)) score(std::true_type(), std::false_type());
+            else if (all_far) score(std::false_type(), std::true_type());
+            else score(std::false_type(), std::false_type());
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                piece<T> sf;
-                as_operand(sf, s[2 * c], s[2 * c + 1]);
+                piece<T> sf[QT];
+#pragma unroll
+                for (int t = 0; t < QT; ++t) as_operand(sf[t], s[t][2 * c], s[t][2 * c + 1]);
 #pragma unroll
                 for (int d = 0; d < MT; ++d) {
                     piece<T> a;
                     K.cols(a, 32 * c, 16 * d);
-                    mma(acc[d], a, sf);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) mma(acc[t][d], a, sf[t]);
                 }
             }
             settle();
             if (part) {
-                int b0 = 0, b1 = 0;
-                bool same = all_far;
-                if (!all_far) {
-                    const int16_t *b = bucket_lds + bias.zero + nearest;          // buckets of the 79 distances
-                    b0 = b[lane];
-                    b1 = lane < 15 ? b[64 + lane] : b0;
-                    const int first = __builtin_amdgcn_readfirstlane(b0);
-                    same = __all(b0 == first && b1 == first);
-                }
-                if (same) {
+                if (all_far) {
                     float share = 0.f;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) share += (s[k][0] + s[k][1]) + (s[k][2] + s[k][3]);
-                    sums.one(all_far ? bucket_lds[far_at] : __builtin_amdgcn_readfirstlane(b0), share);
+                    for (int t = 0; t < QT; ++t)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) share += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
+                    sums.one(__builtin_amdgcn_readfirstlane((int)bucket_lds[far_at]), share);
                 } else {
-                    float near, far;
-                    diagonal_sums(skew + w * kSkew, s, near, far);
-                    sums.each(b0, near);
-                    sums.each(lane < 15 ? b1 : -1, far);
+#pragma unroll
+                    for (int t = QT - 1; t >= 0; --t)
+                        add_by_bucket(sums, skew + w * kSkew, s[t], bucket_lds + bias.zero + near + 16 * t);
                 }
             }
         }
         if (n + 1 < tiles) stage(n + 1);
     }
-    if (live) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int row = wrow + 16 * t + j;
+        if (row >= u.nq) continue;
 #pragma unroll
         for (int c = 0; c < MT; ++c) {
             const int col = 16 * c + 4 * g;
             f32x4 o;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) o[r] = acc[c][r] * p.scale;
+            for (int r = 0; r < 4; ++r) o[r] = acc[t][c][r] * p.scale;
             if (col < p.width) store4(static_cast<T *>(p.dq) + (u.q0 + row) * p.dq_stride + head * p.width + col, o);
         }
     }
@@ -268,7 +342,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dq_kernel(attn_params p) {
 // ---- keys ------------------------------------------------------------------------------------------------------------------------
 // KT: sixteens of keys of a wavefront
 template <typename T, int DH, int KT>
-__global__ __launch_bounds__(kAttnThreads) void attn_dkv_kernel(attn_params p) {
+__global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_kernel(attn_params p) {
     constexpr int kKeys = 16 * kAttnWaves * KT, kShift = KT == 1 ? 6 : 7, kPad = kKeys + kTile;
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
@@ -279,7 +353,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_kernel(attn_params p) {
     uint32_t *odd = reinterpret_cast<uint32_t *>(mark + 4 * kTile);               // [2][wavefronts]
     float *bias_lds = reinterpret_cast<float *>(odd + 2 * kAttnWaves);
 
-    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int kv_heads = p.heads / p.group, kvh = blockIdx.x % kv_heads;
     user u;
     int index;
@@ -381,8 +455,10 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_kernel(attn_params p) {
                 const int nearest = pos0 + 32 * c2 - (wkey + 16 * KT - 1), furthest = pos0 + 32 * c2 + 31 - wkey;
                 const bool all_far = nearest >= bias.high || furthest <= bias.low;
                 const float far = bias.at[bias.zero + (nearest >= bias.high ? bias.high : bias.low)];
-                const float *bb = bias.at + bias.zero + (pos0 + 32 * c2 + 4 * g - wkey - j) - 16 * (KT - 1);
-                const auto score = [&](auto mask) {
+                // of a tile beyond the table, the distances nearest to it have the same bias
+                const int near = min(max(nearest, bias.low - (30 + 16 * KT)), bias.high);
+                const float *bb = bias.at + bias.zero + near + (4 * g - j + 15);
+                const auto score = [&](auto mask, auto away) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int at = 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
@@ -397,7 +473,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_kernel(attn_params p) {
                         for (int t = 0; t < KT; ++t)
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
-                                const float x = all_far ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
+                                const float x = away() ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
                                 float power = s[h][t][r] * scale2 + x - lse[r], d = dp[h][t][r] - delta[r];
                                 if constexpr (mask()) {
                                     // a key that the row does not see, and the keys behind the last
@@ -413,8 +489,9 @@ __global__ __launch_bounds__(kAttnThreads) void attn_dkv_kernel(attn_params p) {
                             }
                     }
                 };
-                if (masked) score(std::true_type());
-                else score(std::false_type());
+                if (masked) score(std::true_type(), std::false_type());
+                else if (all_far) score(std::false_type(), std::true_type());
+                else score(std::false_type(), std::false_type());
 #pragma unroll
                 for (int t = 0; t < KT; ++t) {
                     piece<T> pf, sf;
@@ -513,32 +590,44 @@ constexpr int key_sixteens = sizeof(T) == 2 && DH <= 64 ? 2 : 1;
 
 namespace fs {
 
+// query rows of a wavefront of attn_dq_kernel: as for the keys, where the users have rows for them on average
+static int dq_shift(const attn_params &p, int dt) { return dt == FS_BF16 && p.width <= 64 && p.n_q >= 128 * p.batch ? 7 : 6; }
+
 // scratch: delta, then the bias's sums of every workgroup, then those of the cuts
 static size_t delta_bytes(const attn_params &p) { return ((size_t)p.heads * p.n_q * sizeof(float) + 255) / 256 * 256; }
-static size_t part_bytes(const attn_params &p) {
+static size_t part_bytes(const attn_params &p, int dt) {
     if (!p.dbias) return 0;
-    return ((size_t)attn_slots(p.n_q, p.batch, 6) * p.heads * p.buckets * sizeof(float) + 255) / 256 * 256;
+    return ((size_t)attn_slots(p.n_q, p.batch, dq_shift(p, dt)) * p.heads * p.buckets * sizeof(float) + 255) / 256 * 256;
 }
 
-size_t attention_backward_work(const attn_params &p) {
-    return delta_bytes(p) + part_bytes(p) + (p.dbias ? (size_t)kBiasCuts * p.heads * p.buckets * sizeof(double) : 0);
+size_t attention_backward_work(const attn_params &p, int dt) {
+    return delta_bytes(p) + part_bytes(p, dt) + (p.dbias ? (size_t)kBiasCuts * p.heads * p.buckets * sizeof(double) : 0);
 }
 
 int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void *work, hipStream_t s) {
     attn_params p = args;
     p.delta = static_cast<float *>(work);
     p.bias_part = reinterpret_cast<float *>(static_cast<char *>(work) + delta_bytes(p));
-    double *cut = reinterpret_cast<double *>(static_cast<char *>(work) + delta_bytes(p) + part_bytes(p));
-    const int64_t slots = attn_slots(p.n_q, p.batch, 6);
+    double *cut = reinterpret_cast<double *>(static_cast<char *>(work) + delta_bytes(p) + part_bytes(p, dt));
+    const int shift = dq_shift(p, dt);
+    const int64_t slots = attn_slots(p.n_q, p.batch, shift);
     const bool causal = p.causal != 0;
     if (p.batch > 0) {
         const int rc = by_head(dt, p.width, [&](auto *t, auto dh) -> int {
             using T = std::remove_pointer_t<decltype(t)>;
             constexpr int DH = dh(), KT = key_sixteens<T, DH>, B = tile_buffers<T, DH>;
-            const size_t bias = strip<16 * kAttnWaves + kTile>::entries(p.distances, causal);
-            const size_t rows = 2 * B * sizeof(tile<T, DH>) + (2 * kTile + kAttnWaves * kSkew + bias + kAttnWaves * p.buckets) * sizeof(float) +
-                                (p.dbias ? bias * sizeof(int16_t) : 0);
-            const int done = launch_attention(ctx, attn_dq_kernel<T, DH>, slots * p.heads, rows, s, "attn_dq", p);
+            const auto query_rows = [&](auto qt) {
+                constexpr int QT = qt();
+                const size_t bias = strip<16 * kAttnWaves * QT + kTile>::entries(p.distances, causal);
+                const size_t lds = 2 * B * sizeof(tile<T, DH>) + (2 * kTile + kAttnWaves * kSkew + bias + kAttnWaves * p.buckets) * sizeof(float) +
+                                   (p.dbias ? bias * sizeof(int16_t) : 0);
+                return launch_attention(ctx, attn_dq_kernel<T, DH, QT>, slots * p.heads, lds, s, "attn_dq", p);
+            };
+            int done = FS_OK;
+            if constexpr (key_sixteens<T, DH> == 2)
+                done = shift == 7 ? query_rows(std::integral_constant<int, 2>()) : query_rows(std::integral_constant<int, 1>());
+            else
+                done = query_rows(std::integral_constant<int, 1>());
             if (done != FS_OK) return done;
             const size_t keys = 2 * B * sizeof(tile<T, DH>) + (8 * kTile + 2 * kAttnWaves) * sizeof(float) +
                                 strip<16 * kAttnWaves * KT + kTile>::entries(p.distances, causal) * sizeof(float);
