@@ -96,6 +96,7 @@ size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
 #define FS_MAX_HEAD_DIM 128
 #define FS_MAX_BIAS_BUCKETS 1024
 #define FS_MAX_BIAS_DISTANCES 4096
+#define FS_MAX_ROW_STRIDE (1 << 22)       /* elements */
 
 /* Attention of each user's query rows over the user's keys and values, with a learned bias for the bucket that the distance
  * between the two lies in:
@@ -123,7 +124,7 @@ size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
  *         out are left as they were.
  *   work  fs_jagged_attention_work_bytes(args) bytes, 16-byte aligned, contents irrelevant (0 bytes and NULL but for the form
  *         above)
- * Scores, softmax and sums are in fp32; P and dS are rounded to dt where they go into a product.  head_dim
+ * scale is positive.  Scores, softmax and sums are in fp32; P and dS are rounded to dt where they go into a product.  head_dim
  * a multiple of 4 (fp32) / 8 (bf16), at most FS_MAX_HEAD_DIM.  (rows / 64 + batch) * heads < 2^24, a user has fewer than 2^30 rows.  Boundaries that do not ascend
  * from 0 to n_q (n_kv) and lengths that do not fit their room are reported as FS_ERANGE by fs_check_async; out of the user
  * concerned is not written or is that of the keys there are. */

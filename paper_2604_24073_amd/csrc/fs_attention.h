@@ -155,19 +155,36 @@ __device__ __forceinline__ uint32_t clean_word(uint32_t w, bool &any) {
 template <typename T, int DH>
 constexpr int tile_buffers = sizeof(T) * DH >= 512 ? 1 : 2;
 
+// Rows of a head as the memory unit sees them: what it reads behind the last byte is zeros, and nothing there is touched.
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+struct window {
+    __amdgpu_buffer_rsrc_t r;
+    __device__ __forceinline__ window(const void *base, int64_t bytes)
+        : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(base), 0, (int)bytes, 0x00027000)) {}
+    __device__ __forceinline__ u32x4 load(int offset) const {
+        return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 0));
+    }
+};
+
 // A thread's chunks of the next tile on their way from memory to LDS.
 template <typename T, int DH>
 struct tile_regs {
     u32x4 v[tile<T, DH>::kMine];
-    // rows [0, rows) of base exist, columns [0, width)
-    __device__ __forceinline__ void load(const T *__restrict__ base, int64_t stride, int rows, int width) {
+    int offset[tile<T, DH>::kMine];          // of the thread's chunks from the tile's first row, in bytes; beyond every tile
+                                             // for the columns behind the head's last
+    __device__ __forceinline__ void place(int64_t stride, int width) {
         using t = tile<T, DH>;
 #pragma unroll
         for (int m = 0; m < t::kMine; ++m) {
             const int k = threadIdx.x + kAttnThreads * m, r = k / t::kChunks, c = (k % t::kChunks) * t::kPer;
-            const u32x4 zero = {0u, 0u, 0u, 0u};
-            v[m] = r < rows && c < width ? *reinterpret_cast<const u32x4 *>(base + r * stride + c) : zero;
+            offset[m] = c < width ? (r * (int)stride + c) * (int)sizeof(T) : 0x7FFFFFF0;
         }
+    }
+    // the first `rows` rows from base on exist (any number)
+    __device__ __forceinline__ void load(const T *__restrict__ base, int64_t stride, int rows) {
+        const window w(base, (int64_t)min(max(rows, 0), kTile) * stride * (int)sizeof(T));
+#pragma unroll
+        for (int m = 0; m < tile<T, DH>::kMine; ++m) v[m] = w.load(offset[m]);
     }
     __device__ __forceinline__ void store(tile<T, DH> &to) const {
         using t = tile<T, DH>;

@@ -45,8 +45,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
     const T *vbase = static_cast<const T *>(p.v) + u.k0 * p.v_stride + (head / p.group) * p.width;
 
     tile_regs<T, DH> kr, vr;
-    kr.load(kbase, p.k_stride, tiles ? u.nk : 0, p.width);
-    vr.load(vbase, p.v_stride, tiles ? u.nk : 0, p.width);
+    kr.place(p.k_stride, p.width);
+    vr.place(p.v_stride, p.width);
+    kr.load(kbase, p.k_stride, tiles ? u.nk : 0);
+    vr.load(vbase, p.v_stride, tiles ? u.nk : 0);
 
     // the wavefront's query rows, and where they stand among the keys
     const int wrow = row0 + 16 * QT * w, wpos = u.first + wrow;
@@ -64,11 +66,14 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 
     // the product with P's second term has a sum of its own: an infinity among the values meets a zero or a negative rest there
     f32x4 acc[QT][MT] = {}, acc_rest[EXACT ? QT : 1][MT] = {};
-    float m[QT], l[QT];
+    // m: what the row's scores are less by, where their sums begin (as less, in the product's own terms); it follows the row's
+    // maximum once that is 2^8 ahead, which is enough to keep the powers in range, and at once from the first key seen on
+    float m[QT], l[QT], less[QT], ahead[QT];
+    const float inv_scale2 = 1.f / scale2;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
-        m[t] = neg_inf();
-        l[t] = 0.f;
+        m[t] = l[t] = less[t] = 0.f;
+        ahead[t] = neg_inf();
     }
     // a tile in which some rows do not see all keys: what they do not see must not reach them, not even as 0 * NaN
     const auto edge = [&](int n) { return hides || (p.causal && (n + 1) * kTile - 1 > pos0); };
@@ -86,8 +91,8 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
         __syncthreads();
         const int key0 = n * kTile;
         if (n + 1 < tiles) {
-            kr.load(kbase + (int64_t)(key0 + kTile) * p.k_stride, p.k_stride, u.nk - key0 - kTile, p.width);
-            vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile, p.width);
+            kr.load(kbase + (int64_t)(key0 + kTile) * p.k_stride, p.k_stride, u.nk - key0 - kTile);
+            vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile);
         }
         const tile<T, DH> &K = kt[n & (kBufs - 1)], &V = vt[n & (kBufs - 1)];
         if (wrow < u.nq && !(p.causal && key0 > wpos + 16 * QT - 1)) {
@@ -95,7 +100,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
 #pragma unroll
-                for (int t = 0; t < QT; ++t) s[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < QT; ++t) s[t][k] = f32x4{less[t], less[t], less[t], less[t]};
 #pragma unroll
                 for (int c = 0; c < KC; ++c) {
                     piece<T> a;
@@ -143,12 +148,12 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 #pragma unroll
                     for (int r = 0; r < 4; ++r) top = fmaxf(top, s[t][k][r]);
                 top = column_max(top);
-                // The maximum only has to keep the powers in range: it follows once it is 2^8 behind, each row's by itself.
-                const bool behind = top > m[t] + 8.f;
+                const bool behind = top > ahead[t];
                 if (__any(behind)) {
-                    const float next = behind ? top : m[t];
-                    const float shrink = behind ? __builtin_amdgcn_exp2f(m[t] - next) : 1.f;
-                    m[t] = next;
+                    const float step = behind ? top : 0.f, shrink = behind ? __builtin_amdgcn_exp2f(-step) : 1.f;
+                    m[t] += step;
+                    less[t] = -m[t] * inv_scale2;
+                    ahead[t] = behind ? 8.f : ahead[t];
                     l[t] *= shrink;
 #pragma unroll
                     for (int c = 0; c < MT; ++c)
@@ -157,13 +162,16 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
                             acc[t][c][r] *= shrink;
                             if constexpr (EXACT) acc_rest[t][c][r] *= shrink;
                         }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[t][k][r] -= step;
                 }
-                const float base = m[t] == neg_inf() ? 0.f : m[t];
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        s[t][k][r] = __builtin_amdgcn_exp2f(s[t][k][r] - base);
+                        s[t][k][r] = __builtin_amdgcn_exp2f(s[t][k][r]);
                         l[t] += s[t][k][r];
                     }
             }
@@ -526,7 +534,7 @@ int attn_check(fs_ctx *ctx, const fs_attention_args &a) {
     const int unit = 16 / elem_size(a.dt);
     FS_NEED(a.head_dim > 0 && a.head_dim <= FS_MAX_HEAD_DIM && a.head_dim % unit == 0,
             "jagged attention: head_dim must be a multiple of 4 (fp32) / 8 (bf16), at most FS_MAX_HEAD_DIM");
-    FS_NEED(a.scale > -1e30f && a.scale < 1e30f, "jagged attention: scale is no number of use");
+    FS_NEED(a.scale > 1e-30f && a.scale < 1e30f, "jagged attention: scale must be a positive number");
     FS_NEED(a.causal == 0 || a.causal == 1, "jagged attention: causal must be 0 or 1");
     if (a.bias) {
         FS_NEED(a.bucket_of, "jagged attention: a bias without bucket_of");
@@ -540,6 +548,8 @@ int attn_check(fs_ctx *ctx, const fs_attention_args &a) {
     if (a.batch == 0) return FS_OK;
     FS_NEED(a.q_offsets && a.kv_offsets, "jagged attention: null pointer");
     const int64_t wide = (int64_t)a.heads * a.head_dim, narrow = (int64_t)a.kv_heads * a.head_dim;
+    FS_NEED(a.q_stride <= FS_MAX_ROW_STRIDE && a.k_stride <= FS_MAX_ROW_STRIDE && a.v_stride <= FS_MAX_ROW_STRIDE,
+            "jagged attention: a stride beyond FS_MAX_ROW_STRIDE");
     FS_NEED(a.q_stride >= wide && a.k_stride >= narrow && a.v_stride >= narrow && a.q_stride % unit == 0 && a.k_stride % unit == 0 &&
                 a.v_stride % unit == 0,
             "jagged attention: a stride is less than its row or not a multiple of 16 bytes");

@@ -171,12 +171,15 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
     const T *vbase = static_cast<const T *>(p.v) + u.k0 * p.v_stride + (head / p.group) * p.width;
 
     tile_regs<T, DH> kr, vr;
-    kr.load(kbase, p.k_stride, tiles ? u.nk : 0, p.width);
-    vr.load(vbase, p.v_stride, tiles ? u.nk : 0, p.width);
+    kr.place(p.k_stride, p.width);
+    vr.place(p.v_stride, p.width);
+    kr.load(kbase, p.k_stride, tiles ? u.nk : 0);
+    vr.load(vbase, p.v_stride, tiles ? u.nk : 0);
 
     const int wrow = row0 + 16 * QT * w, wpos = u.first + wrow;
     piece<T> qf[QT][KC], of[QT][KC];
-    float delta[QT], lse2[QT];
+    // what a row's scores and dO V^T are less by is where their sums begin: -lse / scale, -delta
+    float less_s[QT], less_dp[QT];
     const int64_t orow = p.heads * (int64_t)p.width;                              // out and dout are packed
     const int64_t obase = u.q0 * orow + head * p.width;
 #pragma unroll
@@ -198,13 +201,14 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum += o[i] * d[i];
         }
-        delta[t] = column_sum(sum);
-        lse2[t] = __builtin_inff();                                               // a row that sees nothing: P = 0
+        sum = column_sum(sum);
+        less_dp[t] = -sum;
+        less_s[t] = neg_inf();                                                    // a row that sees nothing: P = 0
         if (live) {
             const int64_t at = (int64_t)head * p.n_q + u.q0 + row;
             const float x = p.lse[at];
-            if (x != neg_inf()) lse2[t] = x * kLog2e;
-            if (g == 0) p.delta[at] = delta[t];
+            if (x != neg_inf()) less_s[t] = -x / p.scale;
+            if (g == 0) p.delta[at] = sum;
         }
     }
     strip<kPad> bias;
@@ -231,8 +235,8 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
         __syncthreads();
         const int key0 = n * kTile;
         if (n + 1 < tiles) {
-            kr.load(kbase + (int64_t)(key0 + kTile) * p.k_stride, p.k_stride, u.nk - key0 - kTile, p.width);
-            vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile, p.width);
+            kr.load(kbase + (int64_t)(key0 + kTile) * p.k_stride, p.k_stride, u.nk - key0 - kTile);
+            vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile);
         }
         const tile<T, DH> &K = kt[n & (kBufs - 1)], &V = vt[n & (kBufs - 1)];
         if (wrow < u.nq && !(p.causal && key0 > wpos + 16 * QT - 1)) {
@@ -240,7 +244,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
 #pragma unroll
-                for (int t = 0; t < QT; ++t) s[t][k] = dp[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int t = 0; t < QT; ++t) {
+                    s[t][k] = f32x4{less_s[t], less_s[t], less_s[t], less_s[t]};
+                    dp[t][k] = f32x4{less_dp[t], less_dp[t], less_dp[t], less_dp[t]};
+                }
 #pragma unroll
                 for (int c = 0; c < KC; ++c) {
                     piece<T> a;
@@ -271,7 +278,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float b = away() ? far : bb[51 + 16 * t - 16 * k - r];
-                            float power = s[t][k][r] * scale2 + (b - lse2[t]), d = dp[t][k][r] - delta[t];
+                            float power = s[t][k][r] * scale2 + b, d = dp[t][k][r];
                             if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen ? power + x[r] : neg_inf();
                             const float e = __builtin_amdgcn_exp2f(power);
                             if constexpr (mask()) d = e == 0.f ? 0.f : d;
@@ -348,7 +355,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
     extern __shared__ __align__(16) char lds[];
     constexpr int kBufs = tile_buffers<T, DH>;
     tile<T, DH> *qt = reinterpret_cast<tile<T, DH> *>(lds), *ot = qt + kBufs;
-    float *stats = reinterpret_cast<float *>(ot + kBufs);                         // [2][lse, delta][kTile]
+    float *stats = reinterpret_cast<float *>(ot + kBufs);                         // [2][-lse / scale, -delta][kTile]
     float *mark = stats + 4 * kTile;                                              // [2][q, dout][kTile]
     uint32_t *odd = reinterpret_cast<uint32_t *>(mark + 4 * kTile);               // [2][wavefronts]
     float *bias_lds = reinterpret_cast<float *>(odd + 2 * kAttnWaves);
@@ -379,21 +386,23 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
     }
     f32x4 dk[KT][MT] = {}, dv[KT][MT] = {};
     const int64_t orow = p.heads * (int64_t)p.width;
-    const float scale2 = p.scale * kLog2e;
+    const float scale2 = p.scale * kLog2e, inv_scale = 1.f / p.scale;
     tile_regs<T, DH> qr, dr;
+    qr.place(p.q_stride, p.width);
+    dr.place(orow, p.width);
     float stat = 0.f;
     const auto fetch = [&](int n) {
         const int head = kvh * p.group + n / tiles, r0 = from + (n % tiles) * kTile;
-        qr.load(static_cast<const T *>(p.q) + (u.q0 + r0) * p.q_stride + head * p.width, p.q_stride, u.nq - r0, p.width);
-        dr.load(static_cast<const T *>(p.dout) + (u.q0 + r0) * orow + head * p.width, orow, u.nq - r0, p.width);
+        qr.load(static_cast<const T *>(p.q) + (u.q0 + r0) * p.q_stride + head * p.width, p.q_stride, u.nq - r0);
+        dr.load(static_cast<const T *>(p.dout) + (u.q0 + r0) * orow + head * p.width, orow, u.nq - r0);
         if (threadIdx.x < 2 * kTile) {
             const int r = r0 + (threadIdx.x & (kTile - 1));
             const bool lse = threadIdx.x < kTile;
-            stat = lse ? __builtin_inff() : 0.f;                                  // rows that see nothing and rows that are none
+            stat = lse ? neg_inf() : 0.f;                                         // rows that see nothing and rows that are none
             if (r < u.nq) {
                 const float x = (lse ? p.lse : p.delta)[(int64_t)head * p.n_q + u.q0 + r];
-                if (!lse) stat = x;
-                else if (x != neg_inf()) stat = x * kLog2e;
+                if (!lse) stat = -x;
+                else if (x != neg_inf()) stat = -x * inv_scale;
             }
         }
     };
@@ -438,8 +447,15 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
                 f32x4 s[2][KT], dp[2][KT];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    // what a row's scores and dO V^T are less by is where their sums begin
+                    const float *of_rows = stats + 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
+                    const f32x4 less_s = *reinterpret_cast<const f32x4 *>(of_rows);
+                    const f32x4 less_dp = *reinterpret_cast<const f32x4 *>(of_rows + kTile);
 #pragma unroll
-                    for (int t = 0; t < KT; ++t) s[h][t] = dp[h][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int t = 0; t < KT; ++t) {
+                        s[h][t] = less_s;
+                        dp[h][t] = less_dp;
+                    }
 #pragma unroll
                     for (int c = 0; c < KC; ++c) {
                         piece<T> a;
@@ -462,8 +478,6 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int at = 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
-                        const f32x4 lse = *reinterpret_cast<const f32x4 *>(stats + at);
-                        const f32x4 delta = *reinterpret_cast<const f32x4 *>(stats + kTile + at);
                         f32x4 mq, mo;
                         if constexpr (mask()) {
                             mq = *reinterpret_cast<const f32x4 *>(mark + at);
@@ -474,7 +488,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
 #pragma unroll
                             for (int r = 0; r < 4; ++r) {
                                 const float x = away() ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
-                                float power = s[h][t][r] * scale2 + x - lse[r], d = dp[h][t][r] - delta[r];
+                                float power = s[h][t][r] * scale2 + x, d = dp[h][t][r];
                                 if constexpr (mask()) {
                                     // a key that the row does not see, and the keys behind the last
                                     const int key = wkey + 16 * t + j;

@@ -124,7 +124,7 @@ def heads(**changes):
 ATTENTION = [dict(n_q=-1), dict(n_kv=-1), dict(batch=-1), dict(batch=0), dict(max_q=-1), dict(heads=0), dict(kv_heads=0), dict(heads=3),
              dict(heads=-4, kv_heads=-2), dict(heads=2048, kv_heads=1024, q_stride=1 << 20, k_stride=1 << 20, v_stride=1 << 20),
              dict(head_dim=0), dict(head_dim=36, q_stride=160), dict(head_dim=136, q_stride=1 << 12, k_stride=1 << 12, v_stride=1 << 12),
-             dict(dt=2), dict(scale=float("nan")), dict(scale=float("inf")), dict(causal=2), dict(bucket_of=None), dict(num_buckets=0),
+             dict(dt=2), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=0.0), dict(scale=-0.2), dict(q_stride=(1 << 22) + 8), dict(k_stride=1 << 40), dict(causal=2), dict(bucket_of=None), dict(num_buckets=0),
              dict(num_buckets=1025), dict(num_distances=0), dict(num_distances=4097), dict(n_kv=1 << 31), dict(batch=1 << 31),
              dict(n_q=1 << 62), dict(q_offsets=None), dict(kv_offsets=None), dict(q_stride=120), dict(k_stride=60), dict(v_stride=-64),
              dict(q_stride=132), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q=P + 8), dict(k=P + 2), dict(v=P + 4),
