@@ -379,9 +379,13 @@ struct strip {
     static __host__ __device__ int entries(int distances, bool causal) {
         return (causal ? distances : 2 * distances - 1) + 2 * kPad;
     }
-    // Distances from `from` to `to` (and kPad around) are met.  buckets: also which bucket each distance has, or -1.
-    // Returns whether any bias of them hides (is -inf); has a barrier.
-    __device__ __forceinline__ bool fill(const attn_params &p, int head, float *lds, int from, int to, int16_t *bucket) {
+    // the bucket of a distance, -1 where it is none
+    __device__ __forceinline__ int bucket(const attn_params &p, int d) const {
+        const int k = p.bucket_of[min(max(d, low), high) - low];
+        return k < p.buckets ? max(k, -1) : -1;
+    }
+    // Distances from `from` to `to` (and kPad around) are met.  Returns whether any bias of them hides (is -inf); has a barrier.
+    __device__ __forceinline__ bool fill(const attn_params &p, int head, float *lds, int from, int to) {
         at = lds;
         high = p.distances - 1;
         low = p.causal ? 0 : -high;
@@ -389,20 +393,13 @@ struct strip {
         int a = (from < low ? low : from > high ? high : from) - kPad, b = (to > high ? high : to < low ? low : to) + kPad;
         bool hides = false;
         for (int d = a + (int)threadIdx.x; d <= b; d += kAttnThreads) {
-            const int c = d < low ? low : d > high ? high : d;
             float x = 0.f;
-            int k = -1;
             if (p.bias) {
-                k = p.bucket_of[c - low];
-                if (k < 0 || k >= p.buckets) {
-                    atomicOr(p.flags, kFlagRowRange);
-                    k = -1;
-                } else {
-                    x = p.bias[(int64_t)k * p.heads + head] * kLog2e;
-                }
+                const int k = bucket(p, d);
+                if (k < 0) atomicOr(p.flags, kFlagRowRange);
+                else x = p.bias[(int64_t)k * p.heads + head] * kLog2e;
             }
             at[zero + d] = x;
-            if (bucket) bucket[zero + d] = (int16_t)k;
             hides |= x == neg_inf();
         }
         return __syncthreads_or(hides) != 0;

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
         for (int c = 0; c < KC; ++c) global_rows(qf[t][c], qbase, p.q_stride, row, row < u.nq, 32 * c, p.width);
     }
     strip<kPad> bias;
-    const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last, nullptr);
+    const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last);
     const float scale2 = p.scale * kLog2e;
 
     // the product with P's second term has a sum of its own: an infinity among the values meets a zero or a negative rest there

@@ -99,13 +99,13 @@ __device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], 
     wave_lds_order();
 }
 
-// The 16 x 64 values s of a wavefront, whose distances are 79 that ascend in `buckets`, added to the sums of their buckets.
+// The 16 x 64 values s of a wavefront added to the sums of their buckets; b0: the bucket of the lane's of the first 64 distances,
+// b1: of the 15 behind them, the last one's in the lanes that have none.
 // Tables of distances have few buckets in 79 distances but near zero: one bucket takes every lane's sum as it is, two
 // are told apart by comparing distances, and only more are brought into the order of the distances.  Further distances come
 // first: the tiles go from far to near, and a bucket's lanes are added up when the next bucket begins.
-__device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, const f32x4 (&s)[4], const int16_t *buckets) {
+__device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, const f32x4 (&s)[4], int b0, int b1) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
-    const int b0 = buckets[lane], b1 = buckets[lane < 15 ? 64 + lane : 78];
     const int last0 = __builtin_amdgcn_readlane(b0, 63), before0 = __builtin_amdgcn_update_dpp(b0, b0, 0x138, 0xf, 0xf, false);
     int before1 = __builtin_amdgcn_update_dpp(b1, b1, 0x138, 0xf, 0xf, false);
     before1 = lane == 0 ? last0 : before1;
@@ -148,7 +148,6 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
     float *bias_lds = skew + kAttnWaves * kSkew;
     const int entries = strip<kPad>::entries(p.distances, p.causal != 0);
     float *bins = bias_lds + entries;                                             // [wavefronts][buckets]
-    int16_t *bucket_lds = reinterpret_cast<int16_t *>(bins + kAttnWaves * p.buckets);
 
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int head = blockIdx.x % p.heads;
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
     sums.bins = bins + w * p.buckets;
     if (part)
         for (int b = lane; b < p.buckets; b += kWave) sums.bins[b] = 0.f;
-    const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last, part ? bucket_lds : nullptr);
+    const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last);
     const float scale2 = p.scale * kLog2e;
 
     f32x4 acc[QT][MT] = {};
@@ -240,36 +239,44 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
         }
         const tile<T, DH> &K = kt[n & (kBufs - 1)], &V = vt[n & (kBufs - 1)];
         if (wrow < u.nq && !(p.causal && key0 > wpos + 16 * QT - 1)) {
-            f32x4 s[QT][4], dp[QT][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-#pragma unroll
-                for (int t = 0; t < QT; ++t) {
-                    s[t][k] = f32x4{less_s[t], less_s[t], less_s[t], less_s[t]};
-                    dp[t][k] = f32x4{less_dp[t], less_dp[t], less_dp[t], less_dp[t]};
-                }
-#pragma unroll
-                for (int c = 0; c < KC; ++c) {
-                    piece<T> a;
-                    K.rows(a, 16 * k, 32 * c);
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) mma(s[t][k], a, qf[t][c]);
-                    V.rows(a, 16 * k, 32 * c);
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) mma(dp[t][k], a, of[t][c]);
-                }
-            }
-            // element r of s[t][k]: query row wrow + 16 t + j, key key0 + 16 k + 4 g + r
             const int nearest = wpos - (key0 + kTile - 1), furthest = wpos + 16 * QT - 1 - key0;
             const bool all_far = nearest >= bias.high || furthest <= bias.low;
-            const int far_at = bias.zero + (nearest >= bias.high ? bias.high : bias.low);
-            const float far = bias.at[far_at];
+            const float far = bias.at[bias.zero + (nearest >= bias.high ? bias.high : bias.low)];
             // of a tile beyond the table, the distances nearest to it have the same bias
             const int near = min(max(nearest, bias.low - (62 + 16 * QT)), bias.high);
             const float *bb = bias.at + bias.zero + near + (j - 4 * g) + 12;
-            const auto score = [&](auto mask, auto away) {
+            // the buckets of the distances, on their way while the scores are made
+            int buckets[QT][2];
+            if (part) {
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    buckets[t][0] = bias.bucket(p, near + 16 * t + lane);
+                    buckets[t][1] = bias.bucket(p, near + 16 * t + min(64 + lane, kSpan - 1));
+                }
+            }
+            // element r of s[t][k]: query row wrow + 16 t + j, key key0 + 16 k + 4 g + r
+            f32x4 s[QT][4];
+            // A tile has one form from its first product to its last, so that products run beside powers: mask - some pairs are
+            // not seen, or are none; away - all distances are beyond the table.
+            const auto work = [&](auto mask, auto away) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
+                    f32x4 dp[QT];
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) {
+                        s[t][k] = f32x4{less_s[t], less_s[t], less_s[t], less_s[t]};
+                        dp[t] = f32x4{less_dp[t], less_dp[t], less_dp[t], less_dp[t]};
+                    }
+#pragma unroll
+                    for (int c = 0; c < KC; ++c) {
+                        piece<T> a;
+                        K.rows(a, 16 * k, 32 * c);
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) mma(s[t][k], a, qf[t][c]);
+                        V.rows(a, 16 * k, 32 * c);
+#pragma unroll
+                        for (int t = 0; t < QT; ++t) mma(dp[t], a, of[t][c]);
+                    }
                     f32x4 x;
                     if constexpr (mask()) x = *reinterpret_cast<const f32x4 *>(mark + (n & 1) * kTile + 16 * k + 4 * g);
 #pragma unroll
@@ -278,7 +285,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float b = away() ? far : bb[51 + 16 * t - 16 * k - r];
-                            float power = s[t][k][r] * scale2 + b, d = dp[t][k][r];
+                            float power = s[t][k][r] * scale2 + b, d = dp[t][r];
                             if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen ? power + x[r] : neg_inf();
                             const float e = __builtin_amdgcn_exp2f(power);
                             if constexpr (mask()) d = e == 0.f ? 0.f : d;
@@ -286,24 +293,24 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                         }
                     }
                 }
-            };
-            if (edge(n)) score(std::true_type(), std::false_type());
-            else if (all_far) score(std::false_type(), std::true_type());
-            else score(std::false_type(), std::false_type());
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                piece<T> sf[QT];
+                for (int c = 0; c < 2; ++c) {
+                    piece<T> sf[QT];
 #pragma unroll
-                for (int t = 0; t < QT; ++t) as_operand(sf[t], s[t][2 * c], s[t][2 * c + 1]);
+                    for (int t = 0; t < QT; ++t) as_operand(sf[t], s[t][2 * c], s[t][2 * c + 1]);
 #pragma unroll
-                for (int d = 0; d < MT; ++d) {
-                    piece<T> a;
-                    K.cols(a, 32 * c, 16 * d);
+                    for (int d = 0; d < MT; ++d) {
+                        piece<T> a;
+                        K.cols(a, 32 * c, 16 * d);
 #pragma unroll
-                    for (int t = 0; t < QT; ++t) mma(acc[t][d], a, sf[t]);
+                        for (int t = 0; t < QT; ++t) mma(acc[t][d], a, sf[t]);
+                    }
                 }
-            }
-            settle();
+                settle();
+            };
+            if (edge(n)) work(std::true_type(), std::false_type());
+            else if (all_far) work(std::false_type(), std::true_type());
+            else work(std::false_type(), std::false_type());
             if (part) {
                 if (all_far) {
                     float share = 0.f;
@@ -311,11 +318,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                     for (int t = 0; t < QT; ++t)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) share += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
-                    sums.one(__builtin_amdgcn_readfirstlane((int)bucket_lds[far_at]), share);
+                    sums.one(__builtin_amdgcn_readfirstlane(buckets[0][0]), share);
                 } else {
 #pragma unroll
-                    for (int t = QT - 1; t >= 0; --t)
-                        add_by_bucket(sums, skew + w * kSkew, s[t], bucket_lds + bias.zero + near + 16 * t);
+                    for (int t = QT - 1; t >= 0; --t) add_by_bucket(sums, skew + w * kSkew, s[t], buckets[t][0], buckets[t][1]);
                 }
             }
         }
@@ -408,9 +414,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
     };
     strip<kPad> bias;
     bool hides = false;
-    // some of the tile's rows do not see all keys of the workgroup, or some of those are none
+    // some of the tile's rows do not see all keys of the workgroup, or some of either are none
     const auto edge = [&](int n) {
-        return key_first + kKeys > u.nk || (p.causal && u.first + from + (n % tiles) * kTile < key_first + kKeys - 1);
+        const int r0 = from + (n % tiles) * kTile;
+        return key_first + kKeys > u.nk || r0 + kTile > u.nq || (p.causal && u.first + r0 < key_first + kKeys - 1);
     };
     const auto stage = [&](int n, bool clean) {
         const int b = n & 1;
@@ -425,8 +432,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
         if (threadIdx.x < 2 * kTile) stats[2 * b * kTile + threadIdx.x] = stat;
     };
     const auto fill = [&](int n) {
-        return bias.fill(p, kvh * p.group + n / tiles, bias_lds, u.first + from - (key_first + kKeys - 1), u.first + u.nq - 1 - key_first,
-                         nullptr);
+        return bias.fill(p, kvh * p.group + n / tiles, bias_lds, u.first + from - (key_first + kKeys - 1), u.first + u.nq - 1 - key_first);
     };
     bool masked = false;                      // the tile at hand was cleaned, and is worked on with its marks and masks
     if (turns > 0) {
@@ -440,17 +446,24 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
         const int b = n & 1, r0 = from + (n % tiles) * kTile, pos0 = u.first + r0, head = kvh * p.group + n / tiles;
         if (n + 1 < turns) fetch(n + 1);
         const tile<T, DH> &Q = qt[n & (kBufs - 1)], &O = ot[n & (kBufs - 1)];
-        if (wkey < u.nk && !(p.causal && pos0 + kTile - 1 < wkey)) {
+        // A tile has one form from its first product to its last, so that the products of one half run beside the powers of the
+        // other: mask - some pairs are not seen, or are none; away - all distances are beyond the table.
+        const auto work = [&](auto mask, auto away) {
+            const int nearest = pos0 - (wkey + 16 * KT - 1);
+            const float far = bias.at[bias.zero + (nearest >= bias.high ? bias.high : bias.low)];
 #pragma unroll
             for (int c2 = 0; c2 < 2; ++c2) {                                      // 32 query rows at a time
-                if (r0 + 32 * c2 >= u.nq) break;
+                // element r of s[h][t]: query row r0 + 32 c2 + 16 h + 4 g + r, key wkey + 16 t + j
                 f32x4 s[2][KT], dp[2][KT];
+                // of a tile beyond the table, the distances nearest to it have the same bias
+                const int near = min(max(nearest + 32 * c2, bias.low - (30 + 16 * KT)), bias.high);
+                const float *bb = bias.at + bias.zero + near + (4 * g - j + 15);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     // what a row's scores and dO V^T are less by is where their sums begin
-                    const float *of_rows = stats + 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
-                    const f32x4 less_s = *reinterpret_cast<const f32x4 *>(of_rows);
-                    const f32x4 less_dp = *reinterpret_cast<const f32x4 *>(of_rows + kTile);
+                    const int at = 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
+                    const f32x4 less_s = *reinterpret_cast<const f32x4 *>(stats + at);
+                    const f32x4 less_dp = *reinterpret_cast<const f32x4 *>(stats + kTile + at);
 #pragma unroll
                     for (int t = 0; t < KT; ++t) {
                         s[h][t] = less_s;
@@ -466,62 +479,55 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
 #pragma unroll
                         for (int t = 0; t < KT; ++t) mma(dp[h][t], a, vf[t][c]);
                     }
-                }
-                // element r of s[h][t]: query row r0 + 32 c2 + 16 h + 4 g + r, key wkey + 16 t + j
-                const int nearest = pos0 + 32 * c2 - (wkey + 16 * KT - 1), furthest = pos0 + 32 * c2 + 31 - wkey;
-                const bool all_far = nearest >= bias.high || furthest <= bias.low;
-                const float far = bias.at[bias.zero + (nearest >= bias.high ? bias.high : bias.low)];
-                // of a tile beyond the table, the distances nearest to it have the same bias
-                const int near = min(max(nearest, bias.low - (30 + 16 * KT)), bias.high);
-                const float *bb = bias.at + bias.zero + near + (4 * g - j + 15);
-                const auto score = [&](auto mask, auto away) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int at = 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
-                        f32x4 mq, mo;
-                        if constexpr (mask()) {
-                            mq = *reinterpret_cast<const f32x4 *>(mark + at);
-                            mo = *reinterpret_cast<const f32x4 *>(mark + kTile + at);
-                        }
-#pragma unroll
-                        for (int t = 0; t < KT; ++t)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) {
-                                const float x = away() ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
-                                float power = s[h][t][r] * scale2 + x, d = dp[h][t][r];
-                                if constexpr (mask()) {
-                                    // a key that the row does not see, and the keys behind the last
-                                    const int key = wkey + 16 * t + j;
-                                    const int seen = p.causal ? min(pos0 + 32 * c2 + 16 * h + 4 * g + r + 1, u.nk) : u.nk;
-                                    power = key < seen ? power + mq[r] : neg_inf();
-                                    d += mo[r];
-                                }
-                                const float e = __builtin_amdgcn_exp2f(power);
-                                if constexpr (mask()) d = e == 0.f ? 0.f : d;
-                                s[h][t][r] = e;
-                                dp[h][t][r] = e * d;
-                            }
+                    f32x4 mq, mo;
+                    if constexpr (mask()) {
+                        mq = *reinterpret_cast<const f32x4 *>(mark + at);
+                        mo = *reinterpret_cast<const f32x4 *>(mark + kTile + at);
                     }
-                };
-                if (masked) score(std::true_type(), std::false_type());
-                else if (all_far) score(std::false_type(), std::true_type());
-                else score(std::false_type(), std::false_type());
+#pragma unroll
+                    for (int t = 0; t < KT; ++t)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float x = away() ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
+                            float power = s[h][t][r] * scale2 + x, d = dp[h][t][r];
+                            if constexpr (mask()) {
+                                // a key that the row does not see, the keys behind the last, the rows behind the last
+                                const int key = wkey + 16 * t + j, row = r0 + 32 * c2 + 16 * h + 4 * g + r;
+                                int seen = p.causal ? min(u.first + row + 1, u.nk) : u.nk;
+                                seen = row < u.nq ? seen : 0;
+                                power = key < seen ? power + mq[r] : neg_inf();
+                                d += mo[r];
+                            }
+                            const float e = __builtin_amdgcn_exp2f(power);
+                            if constexpr (mask()) d = e == 0.f ? 0.f : d;
+                            s[h][t][r] = e;
+                            dp[h][t][r] = e * d;
+                        }
+                }
+                piece<T> pf[KT], sf[KT];
 #pragma unroll
                 for (int t = 0; t < KT; ++t) {
-                    piece<T> pf, sf;
-                    as_operand(pf, s[0][t], s[1][t]);
-                    as_operand(sf, dp[0][t], dp[1][t]);
-#pragma unroll
-                    for (int d = 0; d < MT; ++d) {
-                        piece<T> a;
-                        O.cols(a, 32 * c2, 16 * d);
-                        mma(dv[t][d], a, pf);
-                        Q.cols(a, 32 * c2, 16 * d);
-                        mma(dk[t][d], a, sf);
-                    }
+                    as_operand(pf[t], s[0][t], s[1][t]);
+                    as_operand(sf[t], dp[0][t], dp[1][t]);
                 }
-                settle();
+#pragma unroll
+                for (int d = 0; d < MT; ++d) {
+                    piece<T> a;
+                    O.cols(a, 32 * c2, 16 * d);
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) mma(dv[t][d], a, pf[t]);
+                    Q.cols(a, 32 * c2, 16 * d);
+#pragma unroll
+                    for (int t = 0; t < KT; ++t) mma(dk[t][d], a, sf[t]);
+                }
             }
+            settle();
+        };
+        if (wkey < u.nk && !(p.causal && pos0 + kTile - 1 < wkey)) {
+            const int nearest = pos0 - (wkey + 16 * KT - 1), furthest = pos0 + kTile - 1 - wkey;
+            if (masked) work(std::true_type(), std::false_type());
+            else if (nearest >= bias.high || furthest <= bias.low) work(std::false_type(), std::true_type());
+            else work(std::false_type(), std::false_type());
             if (masked) {
                 uint32_t any = 0;
                 for (int x = 0; x < kAttnWaves; ++x) any |= odd[b * kAttnWaves + x];
@@ -633,8 +639,7 @@ int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void
             const auto query_rows = [&](auto qt) {
                 constexpr int QT = qt();
                 const size_t bias = strip<16 * kAttnWaves * QT + kTile>::entries(p.distances, causal);
-                const size_t lds = 2 * B * sizeof(tile<T, DH>) + (2 * kTile + kAttnWaves * kSkew + bias + kAttnWaves * p.buckets) * sizeof(float) +
-                                   (p.dbias ? bias * sizeof(int16_t) : 0);
+                const size_t lds = 2 * B * sizeof(tile<T, DH>) + (2 * kTile + kAttnWaves * kSkew + bias + kAttnWaves * p.buckets) * sizeof(float);
                 return launch_attention(ctx, attn_dq_kernel<T, DH, QT>, slots * p.heads, lds, s, "attn_dq", p);
             };
             int done = FS_OK;
