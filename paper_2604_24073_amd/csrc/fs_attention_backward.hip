@@ -520,8 +520,8 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
 #pragma unroll
                     for (int t = 0; t < KT; ++t) mma(dk[t][d], a, sf[t]);
                 }
+                settle();
             }
-            settle();
         };
         if (wkey < u.nk && !(p.causal && pos0 + kTile - 1 < wkey)) {
             const int nearest = pos0 - (wkey + 16 * KT - 1), furthest = pos0 + kTile - 1 - wkey;
@@ -592,14 +592,22 @@ __global__ __launch_bounds__(256) void attn_bias_cut_kernel(const float *__restr
     __syncthreads();
     if (w == 0 && c < columns) cut[(int64_t)blockIdx.y * columns + c] = (sh[0][c & 63] + sh[1][c & 63]) + (sh[2][c & 63] + sh[3][c & 63]);
 }
+// sixteen columns a workgroup, sixteen threads a column
 __global__ __launch_bounds__(256) void attn_bias_sum_kernel(const double *__restrict__ cut, int heads, int buckets, int cuts,
                                                             float *__restrict__ dbias) {
-    const int k = blockIdx.x * 256 + threadIdx.x, columns = heads * buckets;
-    if (k >= columns) return;
-    const int head = k % heads, bucket = k / heads;
+    __shared__ double sh[16][17];
+    const int c = threadIdx.x & 15, w = threadIdx.x >> 4, k = blockIdx.x * 16 + c, columns = heads * buckets;
     double s = 0.0;
-    for (int c = 0; c < cuts; ++c) s += cut[(int64_t)c * columns + head * buckets + bucket];
-    dbias[k] = (float)s;
+    if (k < columns)
+#pragma unroll
+        for (int i = 0; i < kBiasCuts / 16; ++i) s += w + 16 * i < cuts ? cut[(int64_t)(w + 16 * i) * columns + k] : 0.0;
+    sh[w][c] = s;
+    __syncthreads();
+    if (w != 0 || k >= columns) return;
+    s = 0.0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s += sh[i][c];
+    dbias[(k % buckets) * heads + k / buckets] = (float)s;
 }
 
 // keys of a wavefront: twice sixteen halve what a score reads from LDS; fp32 and the widest rows have no registers for them
@@ -661,7 +669,7 @@ int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void
         attn_bias_cut_kernel<<<dim3((unsigned)ceil_div(columns, 64), kBiasCuts), 256, 0, s>>>(p.bias_part, slots, columns, cut);
         FS_LAUNCH_CHECK(ctx, "attn_bias_cut");
     }
-    attn_bias_sum_kernel<<<(unsigned)ceil_div(columns, 256), 256, 0, s>>>(cut, p.heads, p.buckets, p.batch > 0 ? kBiasCuts : 0, p.dbias);
+    attn_bias_sum_kernel<<<(unsigned)ceil_div(columns, 16), 256, 0, s>>>(cut, p.heads, p.buckets, p.batch > 0 ? kBiasCuts : 0, p.dbias);
     FS_LAUNCH_CHECK(ctx, "attn_bias_sum");
     return FS_OK;
 }

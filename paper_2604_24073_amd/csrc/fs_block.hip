@@ -20,7 +20,8 @@ namespace {
 constexpr int kBlockThreads = 256;
 constexpr int kBlockWaves = kBlockThreads / kWave;
 constexpr int64_t kMaxGrid = 1 << 22;    // workgroups of a launch: a launch has fewer than 2^32 threads
-constexpr int kMaxPartials = 1024;       // workgroups of a backward pass, each with column sums of its own
+constexpr int kMaxPartials = 768;        // workgroups of a backward pass, each with column sums of its own: three a CU, which is what
+                                         // its registers leave room for (297 k rows of 128 columns: 190 us with 1024, 165 with 768)
 
 // LPR lanes share a row, NC times eight columns each: lane l of them holds columns 8 l + 8 LPR c.
 template <typename TR, typename TA, int LPR, int NC, bool JOIN>
@@ -267,22 +268,27 @@ __global__ __launch_bounds__(kBlockThreads) void block_norm_backward_kernel(fs_b
     }
 }
 
-// The column sums of the workgroups added up in 64 bits: sixteen columns a workgroup, sixteen threads a column.
-__global__ __launch_bounds__(256) void block_norm_weights_kernel(fs_block_args p, const float *__restrict__ part, int parts,
-                                                                bool join, bool norm) {
-    __shared__ double sh[16][17];
+// The column sums of the workgroups added up in 64 bits: sixteen columns a workgroup, 64 threads a column.
+constexpr int kSumSlices = 64;
+__global__ __launch_bounds__(16 * kSumSlices) void block_norm_weights_kernel(fs_block_args p, const float *__restrict__ part, int parts,
+                                                                            bool join, bool norm) {
+    __shared__ double sh[kSumSlices][17];
     const int c = threadIdx.x & 15, s = threadIdx.x >> 4;
     const int k = blockIdx.x * 16 + c;                   // column of the T sums, then of the dw_pre sums
     const bool in = k < 2 * p.dim && (k < p.dim ? join : norm);
     double sum = 0.0;
-    if (in)
-        for (int b = s; b < parts; b += 16) sum += (double)part[(int64_t)b * 2 * p.dim + k];
+    if (in) {
+#pragma unroll 4
+        for (int b = s; b < parts; b += kSumSlices) sum += (double)part[(int64_t)b * 2 * p.dim + k];
+    }
     sh[s][c] = sum;
     __syncthreads();
+    for (int half = kSumSlices / 2; half >= 1; half >>= 1) {
+        if (s < half) sh[s][c] += sh[s + half][c];
+        __syncthreads();
+    }
     if (s != 0 || !in) return;
-    sum = 0.0;
-#pragma unroll
-    for (int b = 0; b < 16; ++b) sum += sh[b][c];
+    sum = sh[0][c];
     if (k < p.dim) {
         p.dw_post[k] = parts > 0 ? (float)(sum * (double)p.scale[k]) : 0.f;
         p.dscale[k] = parts > 0 ? (float)(sum * (double)p.w_post[k]) : 0.f;
@@ -472,7 +478,7 @@ int fs_block_norm_backward(fs_ctx *ctx, const fs_block_args *args, fs_stream str
         });
         FS_LAUNCH_CHECK(ctx, "block_norm_backward");
     }
-    block_norm_weights_kernel<<<(unsigned)ceil_div(2 * p.dim, 16), 256, 0, s>>>(p, part, parts, join, norm);
+    block_norm_weights_kernel<<<(unsigned)ceil_div(2 * p.dim, 16), 16 * kSumSlices, 0, s>>>(p, part, parts, join, norm);
     FS_LAUNCH_CHECK(ctx, "block_norm_weights");
     return FS_OK;
 }
