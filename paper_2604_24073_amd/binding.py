@@ -711,48 +711,63 @@ def _ctx_stream(ctx: Context, stream):
     return _stream(torch.cuda.current_stream(ctx.device) if stream is None else stream)
 
 
-def _scratch(ctx: Context, nbytes: int, handle) -> torch.Tensor:
+def _scratch(ctx: Context, like: torch.Tensor, nbytes: int, handle) -> torch.Tensor:
     """Scratch memory that is given back when the call has been enqueued: on the stream of the call, so that what torch makes
     of it next waits for the call."""
-    current = torch.cuda.current_stream(ctx.device)
-    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=f"cuda:{ctx.device}")
-    if handle != (current.cuda_stream or None):
+    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
+    if handle != _ctx_stream(ctx, None):
         work.record_stream(torch.cuda.ExternalStream(handle or 0, device=ctx.device))
     return work
 
 
-def _on(ctx: Context, what: str, *tensors) -> None:
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != ctx.device):
-            raise ValueError(f"{what}: tensor on {t.device}, the context is on cuda:{ctx.device}")
+_DTYPE_CODES = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
 
 
-def _rows2(what: str, t: torch.Tensor, n: int, dim: int, dtype=None, packed: bool = True) -> torch.Tensor:
-    """[n, dim] with its columns next to each other, and its rows too where `packed`."""
-    if t.dim() != 2 or tuple(t.shape) != (n, dim):
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {(n, dim)}")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{what}: {t.dtype}, expected {dtype}")
-    if (dim > 1 and t.stride(1) != 1) or (packed and n > 1 and t.stride(0) != dim):
-        raise ValueError(f"{what}: strides {t.stride()}" + (", a contiguous tensor is needed" if packed else ""))
-    return t
+def _code(what: str, dtype: torch.dtype) -> int:
+    code = _DTYPE_CODES.get(dtype)
+    if code is None:
+        raise TypeError(f"{what}: {dtype}, fp32 or bf16 only")
+    return code
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _addr(what: str, t: torch.Tensor, shape, dtype: torch.dtype, device: int) -> int:
+    """The address of a contiguous tensor of that shape and type on that GPU; raises if it is not one.  (These checks are most
+    of what a small call costs the host: one condition of four quick questions, and the explanation only where one fails.)"""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+        _refuse(what, t, shape, dtype, device)
+    return t.data_ptr()
 
 
-def _weights(what: str, t: torch.Tensor, dim: int) -> torch.Tensor:
-    if t.dtype != torch.float32 or t.numel() != dim or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous fp32 tensor of {dim} values is needed")
-    return t
+def _refuse(what, t, shape, dtype, device):
+    if t.dtype != dtype:
+        raise TypeError(f"{what}: {t.dtype}, {dtype} is needed")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, {tuple(shape)} is needed")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: on {t.device}, the context is on cuda:{device}")
+    raise ValueError(f"{what}: strides {t.stride()}, other than this call takes")
 
 
-def _rows8(what: str, t: Rows8, n: int, dim: int) -> Rows8:
-    if (t.codes.dtype != torch.int8 or t.exps.dtype != torch.uint8 or t.codes.numel() != n * dim
-            or t.exps.numel() * FS_ROWS8_GROUP != n * dim or not t.codes.is_contiguous() or not t.exps.is_contiguous()):
-        raise ValueError(f"{what}: not the {n} x {dim} rows in 8 bits that are expected here")
-    return t
+def _row_addr(what: str, t: torch.Tensor, shape, dtype: torch.dtype, device: int):
+    """(address, elements from row to row) of a tensor whose rows may lie apart; a row itself may not."""
+    if t.is_contiguous():
+        stride = 1
+        for k in shape[1:]:
+            stride *= k
+        return _addr(what, t, shape, dtype, device), stride
+    strides, inner = t.stride(), 1
+    for k in range(len(shape) - 1, 0, -1):
+        if t.dim() != len(shape) or (shape[k] > 1 and strides[k] != inner):
+            _refuse(what, t, shape, dtype, device)
+        inner *= shape[k]
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        _refuse(what, t, shape, dtype, device)
+    return t.data_ptr(), strides[0] if shape[0] > 1 else inner
+
+
+def _pair_addr(what: str, t: Rows8, n: int, dim: int, device: int):
+    return (_addr(what + ".codes", t.codes, (n, dim), torch.int8, device),
+            _addr(what + ".exps", t.exps, (n, dim // FS_ROWS8_GROUP), torch.uint8, device))
 
 
 def _alloc_rows8(n: int, dim: int, device) -> Rows8:
@@ -760,28 +775,34 @@ def _alloc_rows8(n: int, dim: int, device) -> Rows8:
                  torch.empty((n, dim // FS_ROWS8_GROUP), dtype=torch.uint8, device=device))
 
 
+def _matrix(what: str, t: torch.Tensor):
+    if t.dim() != 2:
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, two dimensions are needed")
+    return tuple(t.shape)
+
+
 def fs_rows_pack8(ctx: Context, rows: torch.Tensor, out: Optional[Rows8] = None, stream=None) -> Rows8:
-    n, dim = rows.shape
-    _rows2("rows", rows, n, dim, packed=False)
-    out = _alloc_rows8(n, dim, rows.device) if out is None else _rows8("out", out, n, dim)
-    _on(ctx, "fs_rows_pack8", rows, *out)
-    rc = ctx.lib.fs_rows_pack8(ctx.handle, _ptr(rows), _row_stride(rows), table_dtype_code(rows), n, dim, _ptr(out.codes),
-                               _ptr(out.exps), _ctx_stream(ctx, stream))
-    ctx.check(rc, "fs_rows_pack8")
+    n, dim = _matrix("rows", rows)
+    address, stride = _row_addr("rows", rows, (n, dim), rows.dtype, ctx.device)
+    if out is None:
+        out = _alloc_rows8(n, dim, rows.device)
+    codes, exps = _pair_addr("out", out, n, dim, ctx.device)
+    rc = ctx.lib.fs_rows_pack8(ctx.handle, address, stride, _code("rows", rows.dtype), n, dim, codes, exps, _ctx_stream(ctx, stream))
+    if rc:
+        ctx.check(rc, "fs_rows_pack8")
     return out
 
 
 def fs_rows_unpack8(ctx: Context, packed: Rows8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
                     stream=None) -> torch.Tensor:
-    n, dim = packed.codes.shape
-    _rows8("packed", packed, n, dim)
+    n, dim = _matrix("packed.codes", packed.codes)
+    codes, exps = _pair_addr("packed", packed, n, dim, ctx.device)
     if out is None:
         out = torch.empty((n, dim), dtype=dtype, device=packed.codes.device)
-    _rows2("out", out, n, dim, packed=False)
-    _on(ctx, "fs_rows_unpack8", out, *packed)
-    rc = ctx.lib.fs_rows_unpack8(ctx.handle, _ptr(packed.codes), _ptr(packed.exps), n, dim, _ptr(out), _row_stride(out),
-                                 table_dtype_code(out), _ctx_stream(ctx, stream))
-    ctx.check(rc, "fs_rows_unpack8")
+    address, stride = _row_addr("out", out, (n, dim), out.dtype, ctx.device)
+    rc = ctx.lib.fs_rows_unpack8(ctx.handle, codes, exps, n, dim, address, stride, _code("out", out.dtype), _ctx_stream(ctx, stream))
+    if rc:
+        ctx.check(rc, "fs_rows_unpack8")
     return out
 
 
@@ -791,32 +812,36 @@ def fs_block_norm(ctx: Context, x: torch.Tensor, a: Optional[torch.Tensor] = Non
                   dtype: Optional[torch.dtype] = None, out: Optional[Dict] = None, stream=None) -> Dict:
     """y (where a is given) and h (where w_pre is given); pack: which of "a", "g", "y" are wanted in 8 bits too, as a8, g8,
     y8.  dtype: that of h where there is no a.  `out`: the caller's tensors under the same names."""
-    n, dim = x.shape
-    rec = fs_block_args(n=n, dim=dim, rows_dt=table_dtype_code(x), eps=eps, x=_ptr(_rows2("x", x, n, dim)))
-    given, res = dict(out or {}), {}
-    act = a.dtype if a is not None else dtype or x.dtype
-    wanted = [("y", x.dtype)] if a is not None else []
-    if w_pre is not None:
-        wanted.append(("h", act))
-        rec.w_pre = _ptr(_weights("w_pre", w_pre, dim))
-    for name, dt in wanted:
-        res[name] = _rows2(name, given[name], n, dim, dt) if name in given else torch.empty((n, dim), dtype=dt, device=x.device)
-        setattr(rec, name, _ptr(res[name]))
+    n, dim = shape = _matrix("x", x)
+    dev, rows_dt = ctx.device, x.dtype
+    act = a.dtype if a is not None else dtype or rows_dt
+    rec = fs_block_args()
+    rec.n, rec.dim, rec.eps = n, dim, eps
+    rec.rows_dt, rec.dt = _code("x", rows_dt), _code("a or h", act)
+    rec.x = _addr("x", x, shape, rows_dt, dev)
+    given, res = out or {}, {}
     if a is not None:
-        _rows2("a", a, n, dim, packed=False), _rows2("g", g, n, dim, act, packed=False)
-        rec.a, rec.g, rec.a_stride, rec.g_stride = _ptr(a), _ptr(g), _row_stride(a), _row_stride(g)
-        rec.w_post, rec.scale = _ptr(_weights("w_post", w_post, dim)), _ptr(_weights("scale", scale, dim))
-    rec.dt = table_dtype_code(a if a is not None else res["h"] if "h" in res else x)
+        rec.a, rec.a_stride = _row_addr("a", a, shape, act, dev)
+        rec.g, rec.g_stride = _row_addr("g", g, shape, act, dev)
+        rec.w_post = _addr("w_post", w_post, (dim,), torch.float32, dev)
+        rec.scale = _addr("scale", scale, (dim,), torch.float32, dev)
+        res["y"] = y = given["y"] if "y" in given else torch.empty_like(x)
+        rec.y = _addr("y", y, shape, rows_dt, dev)
+    if w_pre is not None:
+        rec.w_pre = _addr("w_pre", w_pre, (dim,), torch.float32, dev)
+        res["h"] = h = given["h"] if "h" in given else torch.empty(shape, dtype=act, device=x.device)
+        rec.h = _addr("h", h, shape, act, dev)
     for name in pack:
         if name not in ("a", "g", "y") or (a is None and name != "y"):
             raise ValueError(f"pack: no {name!r} to pack")
         key = name + "8"
-        res[key] = _rows8(key, given[key], n, dim) if key in given else _alloc_rows8(n, dim, x.device)
-        setattr(rec, name + "_codes", _ptr(res[key].codes))
-        setattr(rec, name + "_exps", _ptr(res[key].exps))
-    _on(ctx, "fs_block_norm", x, a, g, w_post, scale, w_pre,
-        *(t for v in res.values() for t in (v if isinstance(v, Rows8) else (v,))))
-    ctx.check(ctx.lib.fs_block_norm(ctx.handle, ctypes.byref(rec), _ctx_stream(ctx, stream)), "fs_block_norm")
+        res[key] = packed = given[key] if key in given else _alloc_rows8(n, dim, x.device)
+        codes, exps = _pair_addr(key, packed, n, dim, dev)
+        setattr(rec, name + "_codes", codes)
+        setattr(rec, name + "_exps", exps)
+    rc = ctx.lib.fs_block_norm(ctx.handle, rec, _ctx_stream(ctx, stream))
+    if rc:
+        ctx.check(rc, "fs_block_norm")
     return res
 
 
@@ -829,110 +854,89 @@ def fs_block_norm_backward(ctx: Context, dy: Optional[torch.Tensor], dh: Optiona
     """dx, and da, dg, dw_post, dscale where a is given, dw_pre where dh is given.  a, g, y: as the forward pass had or left
     them, or its a8, g8, y8.  dtype, rows_dtype: those of the block's rows and of the residual rows, where no tensor given
     tells."""
-    some = next(t for t in (dy, dh, a, y) if t is not None)
-    shape = some.codes.shape if isinstance(some, Rows8) else some.shape
-    n, dim = shape
-    device = some.codes.device if isinstance(some, Rows8) else some.device
+    some = dy if dy is not None else dh if dh is not None else a if a is not None else y
+    if isinstance(some, Rows8):
+        some = some.codes
+    n, dim = shape = _matrix("dy, dh, a or y", some)
+    dev, device, f32 = ctx.device, some.device, torch.float32
     plain = lambda *ts: next((t.dtype for t in ts if isinstance(t, torch.Tensor)), None)  # noqa: E731
-    rows_dt = plain(dy, y) or rows_dtype or torch.float32
+    rows_dt = plain(dy, y) or rows_dtype or f32
     act = plain(dh, a, g) or dtype or rows_dt
-    codes = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
-    if rows_dt not in codes or act not in codes:
-        raise TypeError(f"{rows_dt}, {act}: fp32 or bf16 only")
-    rec = fs_block_args(n=n, dim=dim, rows_dt=codes[rows_dt], dt=codes[act], eps=eps)
-    given, res, used = dict(out or {}), {}, [dy, dh]
-
-    def output(name, shape, dt):
-        t = given[name] if name in given else torch.empty(shape, dtype=dt, device=device)
-        if len(shape) == 1:
-            _weights(name, t, shape[0])
-        else:
-            _rows2(name, t, n, dim, dt, packed=name == "dx")
-        res[name] = t
-        setattr(rec, name, _ptr(t))
-
-    def kept(name, t, dt, packed):
-        if isinstance(t, Rows8):
-            _rows8(name, t, n, dim)
-            setattr(rec, name + "_codes", _ptr(t.codes))
-            setattr(rec, name + "_exps", _ptr(t.exps))
-            used.extend(t)
-            return
-        _rows2(name, t, n, dim, dt, packed=packed)
-        setattr(rec, name, _ptr(t))
-        used.append(t)
-
-    output("dx", (n, dim), rows_dt)
+    rec = fs_block_args()
+    rec.n, rec.dim, rec.eps = n, dim, eps
+    rec.rows_dt, rec.dt = _code("dy or y", rows_dt), _code("dh, a or g", act)
+    given, res = out or {}, {}
+    res["dx"] = t = given["dx"] if "dx" in given else torch.empty(shape, dtype=rows_dt, device=device)
+    rec.dx = _addr("dx", t, shape, rows_dt, dev)
     if dy is not None:
-        rec.dy = _ptr(_rows2("dy", dy, n, dim, rows_dt))
+        rec.dy = _addr("dy", dy, shape, rows_dt, dev)
     if dh is not None:
-        rec.dh = _ptr(_rows2("dh", dh, n, dim, act))
-        rec.w_pre = _ptr(_weights("w_pre", w_pre, dim))
-        kept("y", y, rows_dt, True)
-        output("dw_pre", (dim,), torch.float32)
+        rec.dh = _addr("dh", dh, shape, act, dev)
+        rec.w_pre = _addr("w_pre", w_pre, (dim,), f32, dev)
+        if isinstance(y, Rows8):
+            rec.y_codes, rec.y_exps = _pair_addr("y", y, n, dim, dev)
+        else:
+            rec.y = _addr("y", y, shape, rows_dt, dev)
+        res["dw_pre"] = t = given["dw_pre"] if "dw_pre" in given else torch.empty_like(w_pre)
+        rec.dw_pre = _addr("dw_pre", t, (dim,), f32, dev)
     if a is not None:
-        kept("a", a, act, False)
-        kept("g", g, act, False)
-        rec.a_stride = _row_stride(a) if isinstance(a, torch.Tensor) else 0
-        rec.g_stride = _row_stride(g) if isinstance(g, torch.Tensor) else 0
-        rec.w_post, rec.scale = _ptr(_weights("w_post", w_post, dim)), _ptr(_weights("scale", scale, dim))
-        for name in ("da", "dg"):
-            output(name, (n, dim), act)
-        rec.da_stride, rec.dg_stride = _row_stride(res["da"]), _row_stride(res["dg"])
-        for name in ("dw_post", "dscale"):
-            output(name, (dim,), torch.float32)
-    _on(ctx, "fs_block_norm_backward", *used, w_post if a is not None else None, scale if a is not None else None,
-        w_pre if dh is not None else None, *res.values())
+        if isinstance(a, Rows8):
+            rec.a_codes, rec.a_exps = _pair_addr("a", a, n, dim, dev)
+        else:
+            rec.a, rec.a_stride = _row_addr("a", a, shape, act, dev)
+        if isinstance(g, Rows8):
+            rec.g_codes, rec.g_exps = _pair_addr("g", g, n, dim, dev)
+        else:
+            rec.g, rec.g_stride = _row_addr("g", g, shape, act, dev)
+        rec.w_post = _addr("w_post", w_post, (dim,), f32, dev)
+        rec.scale = _addr("scale", scale, (dim,), f32, dev)
+        res["da"] = t = given["da"] if "da" in given else torch.empty(shape, dtype=act, device=device)
+        rec.da, rec.da_stride = _row_addr("da", t, shape, act, dev)
+        res["dg"] = t = given["dg"] if "dg" in given else torch.empty(shape, dtype=act, device=device)
+        rec.dg, rec.dg_stride = _row_addr("dg", t, shape, act, dev)
+        res["dw_post"] = t = given["dw_post"] if "dw_post" in given else torch.empty_like(w_post)
+        rec.dw_post = _addr("dw_post", t, (dim,), f32, dev)
+        res["dscale"] = t = given["dscale"] if "dscale" in given else torch.empty_like(scale)
+        rec.dscale = _addr("dscale", t, (dim,), f32, dev)
     handle = _ctx_stream(ctx, stream)
-    nbytes = ctx.lib.fs_block_norm_work_bytes(n, dim)
-    work = _scratch(ctx, nbytes, handle)
-    rec.work, rec.work_bytes = _ptr(work), work.numel()
-    ctx.check(ctx.lib.fs_block_norm_backward(ctx.handle, ctypes.byref(rec), handle), "fs_block_norm_backward")
+    work = _scratch(ctx, some, ctx.lib.fs_block_norm_work_bytes(n, dim), handle)
+    rec.work, rec.work_bytes = work.data_ptr(), work.numel()
+    rc = ctx.lib.fs_block_norm_backward(ctx.handle, rec, handle)
+    if rc:
+        ctx.check(rc, "fs_block_norm_backward")
     return res
 
 
-FS_MAX_HEAD_DIM, FS_MAX_BIAS_BUCKETS, FS_MAX_BIAS_DISTANCES = 128, 1024, 4096
+FS_MAX_HEAD_DIM, FS_MAX_BIAS_BUCKETS, FS_MAX_BIAS_DISTANCES, FS_MAX_ROW_STRIDE = 128, 1024, 4096, 1 << 22
 
 
-def _heads(what: str, t: torch.Tensor, shape=None, dtype=None, packed: bool = False) -> int:
-    """The row stride of a [rows, heads, head_dim] tensor whose heads lie next to each other."""
-    if t.dim() != 3 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{what}: shape {tuple(t.shape)}, expected {'[rows, heads, head_dim]' if shape is None else tuple(shape)}")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{what}: {t.dtype}, expected {dtype}")
-    n, heads, width = t.shape
-    if (width > 1 and t.stride(2) != 1) or (heads > 1 and t.stride(1) != width) or (packed and n > 1 and t.stride(0) != heads * width):
-        raise ValueError(f"{what}: strides {t.stride()}" + (", a contiguous tensor is needed" if packed else ""))
-    return t.stride(0) if n > 1 else heads * width
-
-
-def _index(what: str, t: torch.Tensor, dtype: torch.dtype, size: Optional[int] = None) -> torch.Tensor:
-    if t.dtype != dtype or t.dim() != 1 or not t.is_contiguous() or (size is not None and t.numel() != size):
-        raise ValueError(f"{what}: a contiguous {dtype} tensor" + (f" of {size} values" if size is not None else "") + " is needed")
-    return t
-
-
-def _attention_record(q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale):
-    n_q, heads, width = q.shape if q.dim() == 3 else (0, 0, 0)
-    n_kv, kv_heads = k.shape[0], k.shape[1] if k.dim() == 3 else 0
-    batch = q_offsets.numel() - 1
-    rec = fs_attention_args(
-        q=_ptr(q), k=_ptr(k), v=_ptr(v), q_stride=_heads("q", q), k_stride=_heads("k", k, (n_kv, kv_heads, width), q.dtype),
-        v_stride=_heads("v", v, (n_kv, kv_heads, width), q.dtype), n_q=n_q, n_kv=n_kv, batch=batch,
-        q_offsets=_ptr(_index("q_offsets", q_offsets, torch.int64)), heads=heads, kv_heads=kv_heads, head_dim=width,
-        kv_offsets=_ptr(_index("kv_offsets", kv_offsets, torch.int64, batch + 1)), dt=table_dtype_code(q), causal=int(causal),
-        scale=width ** -0.5 if scale is None and width else scale or 0.0)
+def _attention_record(ctx, q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale):
+    """The record of a call but for what it writes; (shape of q, of k and v)."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError(f"q, k: shapes {tuple(q.shape)}, {tuple(k.shape)}, [rows, heads, head_dim] are needed")
+    dev, dt, i64 = ctx.device, q.dtype, torch.int64
+    shape, (n_kv, kv_heads, _) = tuple(q.shape), k.shape
+    n_q, heads, width = shape
+    keys, users = (n_kv, kv_heads, width), (q_offsets.numel(),)
+    rec = fs_attention_args()
+    rec.dt = _code("q", dt)
+    rec.q, rec.q_stride = _row_addr("q", q, shape, dt, dev)
+    rec.k, rec.k_stride = _row_addr("k", k, keys, dt, dev)
+    rec.v, rec.v_stride = _row_addr("v", v, keys, dt, dev)
+    rec.n_q, rec.n_kv, rec.batch, rec.heads, rec.kv_heads, rec.head_dim = n_q, n_kv, users[0] - 1, heads, kv_heads, width
+    rec.q_offsets = _addr("q_offsets", q_offsets, users, i64, dev)
+    rec.kv_offsets = _addr("kv_offsets", kv_offsets, users, i64, dev)
+    rec.causal, rec.scale = 1 if causal else 0, width ** -0.5 if scale is None and width else scale or 0.0
     if kv_lengths is not None:
-        rec.kv_lengths = _ptr(_index("kv_lengths", kv_lengths, torch.int64, batch))
+        rec.kv_lengths = _addr("kv_lengths", kv_lengths, (users[0] - 1,), i64, dev)
     if bias is not None:
-        if bias.dtype != torch.float32 or bias.dim() != 2 or bias.shape[1] != heads or not bias.is_contiguous():
-            raise ValueError(f"bias: a contiguous fp32 tensor [buckets, {heads}] is needed")
-        size = _index("bucket_of", bucket_of, torch.int32).numel()
+        buckets, size = bias.shape[0], bucket_of.numel()
         if not causal and size % 2 == 0:
             raise ValueError(f"bucket_of: {size} entries, an odd number is needed for distances on both sides")
-        rec.bias, rec.bucket_of, rec.num_buckets = _ptr(bias), _ptr(bucket_of), bias.shape[0]
-        rec.num_distances = size if causal else (size + 1) // 2
-    return rec
+        rec.bias = _addr("bias", bias, (buckets, heads), torch.float32, dev)
+        rec.bucket_of = _addr("bucket_of", bucket_of, (size,), torch.int32, dev)
+        rec.num_buckets, rec.num_distances = buckets, size if causal else (size + 1) // 2
+    return rec, shape, keys
 
 
 def fs_jagged_attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
@@ -942,33 +946,26 @@ def fs_jagged_attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch
                         stream=None) -> Dict[str, torch.Tensor]:
     """out [n_q, heads, head_dim]; keep: also what fs_jagged_attention_backward reads (lse, and out_f32 of bf16 rows).  scale:
     1 / sqrt(head_dim) unless given.  `out`: the caller's tensors under the same names."""
-    rec = _attention_record(q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale)
+    rec, shape, _ = _attention_record(ctx, q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale)
     rec.max_q = max_q
-    given, res = dict(out or {}), {}
-    shape = (rec.n_q, rec.heads, rec.head_dim)
-    wanted = {"out": q.dtype}
-    if keep or "out_f32" in given:
-        wanted["out_f32"] = torch.float32
-    for name, dt in wanted.items():
-        if name == "out_f32" and q.dtype == torch.float32:
-            continue
-        t = given[name] if name in given else torch.empty(shape, dtype=dt, device=q.device)
-        _heads(name, t, shape, dt, packed=True)
-        res[name] = t
-        setattr(rec, name, _ptr(t))
+    given, res, dev, f32 = out or {}, {}, ctx.device, torch.float32
+    res["out"] = t = given["out"] if "out" in given else torch.empty(shape, dtype=q.dtype, device=q.device)
+    rec.out = _addr("out", t, shape, q.dtype, dev)
+    if (keep or "out_f32" in given) and q.dtype != f32:
+        res["out_f32"] = t = given["out_f32"] if "out_f32" in given else torch.empty(shape, dtype=f32, device=q.device)
+        rec.out_f32 = _addr("out_f32", t, shape, f32, dev)
     if keep or "lse" in given:
-        t = given["lse"] if "lse" in given else torch.empty((rec.heads, rec.n_q), dtype=torch.float32, device=q.device)
-        if t.dtype != torch.float32 or tuple(t.shape) != (rec.heads, rec.n_q) or not t.is_contiguous():
-            raise ValueError(f"lse: a contiguous fp32 tensor [{rec.heads}, {rec.n_q}] is needed")
-        res["lse"], rec.lse = t, _ptr(t)
-    _on(ctx, "fs_jagged_attention", q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, *res.values())
+        res["lse"] = t = given["lse"] if "lse" in given else torch.empty((shape[1], shape[0]), dtype=f32, device=q.device)
+        rec.lse = _addr("lse", t, (shape[1], shape[0]), f32, dev)
     handle = _ctx_stream(ctx, stream)
     if max_q:
-        nbytes = ctx.lib.fs_jagged_attention_work_bytes(ctypes.byref(rec))
+        nbytes = ctx.lib.fs_jagged_attention_work_bytes(rec)
         if nbytes:
-            work = _scratch(ctx, nbytes, handle)
-            rec.work, rec.work_bytes = _ptr(work), work.numel()
-    ctx.check(ctx.lib.fs_jagged_attention(ctx.handle, ctypes.byref(rec), handle), "fs_jagged_attention")
+            work = _scratch(ctx, q, nbytes, handle)
+            rec.work, rec.work_bytes = work.data_ptr(), work.numel()
+    rc = ctx.lib.fs_jagged_attention(ctx.handle, rec, handle)
+    if rc:
+        ctx.check(rc, "fs_jagged_attention")
     return res
 
 
@@ -979,33 +976,27 @@ def fs_jagged_attention_backward(ctx: Context, dout: torch.Tensor, kept: Dict[st
                                  out: Optional[Dict[str, torch.Tensor]] = None, stream=None) -> Dict[str, torch.Tensor]:
     """dq, dk, dv, and dbias where there is a bias.  kept: what fs_jagged_attention(keep=True) returned.  `out`: the caller's
     tensors under the same names."""
-    rec = _attention_record(q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale)
-    shape, keys = (rec.n_q, rec.heads, rec.head_dim), (rec.n_kv, rec.kv_heads, rec.head_dim)
-    _heads("dout", dout, shape, q.dtype, packed=True)
-    _heads("kept['out']", kept["out"], shape, q.dtype, packed=True)
-    rec.dout, rec.out = _ptr(dout), _ptr(kept["out"])
-    lse, exact = kept["lse"], kept.get("out_f32")
-    if lse.dtype != torch.float32 or tuple(lse.shape) != (rec.heads, rec.n_q) or not lse.is_contiguous():
-        raise ValueError(f"kept['lse']: a contiguous fp32 tensor [{rec.heads}, {rec.n_q}] is needed")
-    rec.lse = _ptr(lse)
-    if exact is not None:
-        _heads("kept['out_f32']", exact, shape, torch.float32, packed=True)
-        rec.out_f32 = _ptr(exact)
-    given, res = dict(out or {}), {}
-    for name, dims in (("dq", shape), ("dk", keys), ("dv", keys)):
-        t = given[name] if name in given else torch.empty(dims, dtype=q.dtype, device=q.device)
-        setattr(rec, name + "_stride", _heads(name, t, dims, q.dtype))
-        setattr(rec, name, _ptr(t))
-        res[name] = t
+    rec, shape, keys = _attention_record(ctx, q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale)
+    dev, dt, f32 = ctx.device, q.dtype, torch.float32
+    rec.dout = _addr("dout", dout, shape, dt, dev)
+    rec.out = _addr("kept['out']", kept["out"], shape, dt, dev)
+    rec.lse = _addr("kept['lse']", kept["lse"], (shape[1], shape[0]), f32, dev)
+    if kept.get("out_f32") is not None:
+        rec.out_f32 = _addr("kept['out_f32']", kept["out_f32"], shape, f32, dev)
+    given, res = out or {}, {}
+    res["dq"] = t = given["dq"] if "dq" in given else torch.empty(shape, dtype=dt, device=q.device)
+    rec.dq, rec.dq_stride = _row_addr("dq", t, shape, dt, dev)
+    res["dk"] = t = given["dk"] if "dk" in given else torch.empty(keys, dtype=dt, device=q.device)
+    rec.dk, rec.dk_stride = _row_addr("dk", t, keys, dt, dev)
+    res["dv"] = t = given["dv"] if "dv" in given else torch.empty(keys, dtype=dt, device=q.device)
+    rec.dv, rec.dv_stride = _row_addr("dv", t, keys, dt, dev)
     if bias is not None:
-        t = given["dbias"] if "dbias" in given else torch.empty_like(bias)
-        if t.dtype != torch.float32 or t.shape != bias.shape or not t.is_contiguous():
-            raise ValueError(f"dbias: a contiguous fp32 tensor {tuple(bias.shape)} is needed")
-        res["dbias"], rec.dbias = t, _ptr(t)
-    _on(ctx, "fs_jagged_attention_backward", dout, kept["out"], lse, exact, q, k, v, q_offsets, kv_offsets, bias, bucket_of,
-        kv_lengths, *res.values())
+        res["dbias"] = t = given["dbias"] if "dbias" in given else torch.empty_like(bias)
+        rec.dbias = _addr("dbias", t, bias.shape, f32, dev)
     handle = _ctx_stream(ctx, stream)
-    work = _scratch(ctx, ctx.lib.fs_jagged_attention_backward_work_bytes(ctypes.byref(rec)), handle)
-    rec.work, rec.work_bytes = _ptr(work), work.numel()
-    ctx.check(ctx.lib.fs_jagged_attention_backward(ctx.handle, ctypes.byref(rec), handle), "fs_jagged_attention_backward")
+    work = _scratch(ctx, q, ctx.lib.fs_jagged_attention_backward_work_bytes(rec), handle)
+    rec.work, rec.work_bytes = work.data_ptr(), work.numel()
+    rc = ctx.lib.fs_jagged_attention_backward(ctx.handle, rec, handle)
+    if rc:
+        ctx.check(rc, "fs_jagged_attention_backward")
     return res
