@@ -94,14 +94,13 @@ __device__ __forceinline__ void as_operands(piece<float> &p, piece<float> &, con
 // ---- tiles in LDS -------------------------------------------------------------------------------------------------------------
 // kTile rows of DH columns (the head's width rounded up to 32, 64 or 128; zeros behind it), rows 16 bytes further apart than
 // they are long: sixteen lanes that read 16 bytes each of neighbouring rows find them in different banks.
-template <typename T, int DH>
+template <typename T, int DH, int ROWS = kTile>
 struct tile {
     static constexpr int kLd = DH + 16 / (int)sizeof(T);
     static constexpr int kPer = 16 / (int)sizeof(T);              // elements of a 16-byte chunk
     static constexpr int kChunks = DH / kPer;                     // chunks of a row
-    static constexpr int kMine = kTile * kChunks / kAttnThreads;  // chunks of a thread
-    static_assert(kMine >= 1, "a tile has at least one chunk for every thread");
-    T at[kTile * kLd];
+    static constexpr int kMine = ROWS * kChunks / kAttnThreads;   // chunks of a thread of a workgroup
+    T at[ROWS * kLd];
 
     // A over columns: rows row0 + j, columns col0 + 8 g + i
     __device__ __forceinline__ void rows(piece<T> &p, int row0, int col0) const {
@@ -169,6 +168,7 @@ struct window {
 // A thread's chunks of the next tile on their way from memory to LDS.
 template <typename T, int DH>
 struct tile_regs {
+    static_assert(tile<T, DH>::kMine >= 1, "a tile has at least one chunk for every thread");
     u32x4 v[tile<T, DH>::kMine];
     int offset[tile<T, DH>::kMine];          // of the thread's chunks from the tile's first row, in bytes; beyond every tile
                                              // for the columns behind the head's last
@@ -324,10 +324,8 @@ __device__ __forceinline__ int last_user(const int64_t *__restrict__ offsets, in
     return lo;
 }
 
-// The rows in use of a user with so many rows: lengths[b], brought into [0, room].
-__device__ __forceinline__ int rows_in_use(const int64_t *__restrict__ lengths, int64_t b, int room) {
-    if (!lengths) return room;
-    const int64_t used = lengths[b];
+// The rows in use of a user with so many rows, brought into [0, room].
+__device__ __forceinline__ int rows_in_use(int64_t used, int room) {
     const int high = (int)(used >> 32), low = (int)used;
     const int some = high > 0 ? room : low < 0 ? room : min(low, room);
     return high < 0 ? 0 : some;
@@ -342,22 +340,24 @@ __device__ __forceinline__ bool find_user(const attn_params &p, const int64_t *_
     const int lo = last_user(offsets, (int)p.batch, shift, 1, slot);
     u.b = lo;
     const int64_t qa = p.q_offsets[lo], qb = p.q_offsets[lo + 1], ka = p.kv_offsets[lo], kb = p.kv_offsets[lo + 1];
+    const int64_t used = p.kv_lengths ? p.kv_lengths[lo] : kb - ka;                // asked for with the boundaries
     if (qa < 0 || qb < qa || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv || qb - qa > 0x3fffffff || kb - ka > 0x3fffffff)
         return false;
     u.q0 = qa;
     u.k0 = ka;
     u.nq = (int)(qb - qa);
     u.room = (int)(kb - ka);
-    u.nk = rows_in_use(p.kv_lengths, lo, u.room);
+    u.nk = rows_in_use(used, u.room);
     u.first = u.nk - u.nq;
     const int64_t k = slot - ((offsets[lo] >> shift) + lo);
     index = (int)k;
     return k >= 0 && k < 0x3fffffff;
 }
 
-// Thread by thread over the whole grid: offsets that do not ascend from 0 to the number of rows, lengths beyond their room.
-__device__ __forceinline__ void check_layout(const attn_params &p, int64_t group) {
-    for (int64_t b = group * kAttnThreads + threadIdx.x; b < p.batch; b += (int64_t)gridDim.x * kAttnThreads) {
+// Thread by thread over the slots, the last slots first, which often have no tile to work on: offsets that do not ascend from 0
+// to the number of rows, lengths beyond their room.
+__device__ __forceinline__ void check_layout(const attn_params &p, int slot, int slots) {
+    for (int64_t b = (int64_t)(slots - 1 - slot) * kAttnThreads + threadIdx.x; b < p.batch; b += (int64_t)slots * kAttnThreads) {
         const int64_t qa = p.q_offsets[b], qb = p.q_offsets[b + 1], ka = p.kv_offsets[b], kb = p.kv_offsets[b + 1];
         bool bad = qa < 0 || qb < qa || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv;
         bad |= b == 0 && (qa != 0 || ka != 0);

@@ -32,7 +32,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int head = blockIdx.x % p.heads;
     const int slot = (int)(blockIdx.x / p.heads);
-    if (head == 0) check_layout(p, slot);
+    if (head == 0) check_layout(p, slot, (int)(gridDim.x / p.heads));
     user u;
     int index;
     if (!find_user(p, p.q_offsets, slot, kShift, u, index) || (int64_t)index * kRows >= u.nq) return;
@@ -255,20 +255,30 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 // columns of a product), its wavefronts take 64 keys each in turn, and what they have of m, l and o is put together, in the
 // workgroup first, then, where a user has several chunks, by a second launch.
 constexpr int kSplitCols = 16;
-constexpr int kSplitStep = kAttnWaves * kTile;        // keys of a workgroup at a time
+constexpr int kSplitKeys = 32;                        // keys of a wavefront at a time
+constexpr int kSplitStep = kAttnWaves * kSplitKeys;   // keys of a workgroup at a time
+
+// bytes of LDS for the wavefronts' rows of v, and afterwards for what they have of the result: m, l and rows of DH + 4
+template <typename T, int DH>
+constexpr int split_rows_lds = kAttnWaves * (sizeof(tile<T, DH, kSplitKeys>) > 4 * kSplitCols * (DH + 6)
+                                                 ? (int)sizeof(tile<T, DH, kSplitKeys>) : 4 * kSplitCols * (DH + 6));
+// Wavefronts of a SIMD: all of a serving batch's workgroups want to be under way at once, since each is one chain of waits
+template <typename T, int DH>
+constexpr int split_waves = sizeof(T) * DH <= 64 ? 5 : sizeof(T) * DH <= 128 ? 4 : sizeof(T) * DH <= 256 ? 2 : 1;
 
 template <typename T, int DH>
-__global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_split_kernel(attn_params p) {
+__global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split_kernel(attn_params p) {
     const int shift = p.split_shift, max_q = p.max_q;
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
-    tile<T, DH> *vt = reinterpret_cast<tile<T, DH> *>(lds);                                   // [wavefronts]
+    using vtile = tile<T, DH, kSplitKeys>;
+    vtile *vt = reinterpret_cast<vtile *>(lds);                                               // [wavefronts]
     float *merge = reinterpret_cast<float *>(lds);                                            // the same memory, afterwards
-    float *bias_lds = reinterpret_cast<float *>(lds + kAttnWaves * sizeof(tile<T, DH>));
+    float *bias_lds = reinterpret_cast<float *>(lds + split_rows_lds<T, DH>);
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int kv_heads = p.heads / p.group, kvh = blockIdx.x % kv_heads;
     const int slot = (int)(blockIdx.x / kv_heads);
-    if (kvh == 0) check_layout(p, slot);
+    if (kvh == 0) check_layout(p, slot, (int)(gridDim.x / kv_heads));
     user u;
     int index;
     if (!find_user(p, p.kv_offsets, slot, shift, u, index)) return;
@@ -294,44 +304,44 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_split_
 
     f32x4 acc[MT] = {};
     float m = neg_inf(), l = 0.f;
+    const int met = kSplitStep + u.nq - 1;                // distances of a step's keys from the query rows
     for (int step = begin; step < stop; step += kSplitStep) {
-        const int key0 = step + kTile * w, keys = stop - key0 < kTile ? stop - key0 : kTile;   // of the wavefront; may be none
-        piece<T> kf[4][KC];
+        const int key0 = step + kSplitKeys * w, keys = stop - key0 < kSplitKeys ? stop - key0 : kSplitKeys;   // of the wavefront; may be none
+        // from the last key's distance to the first's: their buckets on the way first, the biases behind the rows of k and v
+        const int from = u.first - (step + kSplitStep - 1);
+        const int bucket = p.bias ? p.bucket_of[min(max(from + (int)threadIdx.x, low), high) - low] : 0;
+        piece<T> kf[kSplitKeys / 16][KC];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
+        for (int k = 0; k < kSplitKeys / 16; ++k)
 #pragma unroll
             for (int c = 0; c < KC; ++c)
                 global_rows(kf[k][c], kbase + (int64_t)key0 * p.k_stride, p.k_stride, 16 * k + j, 16 * k + j < keys, 32 * c, p.width);
         // the wavefront's rows of v: the lanes take the chunks of 16 bytes one after the other
-        using vtile = tile<T, DH>;
-        u32x4 vv[vtile::kChunks];
+        constexpr int kMine = vtile::kChunks * kSplitKeys / kWave;
+        u32x4 vv[kMine];
 #pragma unroll
-        for (int x = 0; x < vtile::kChunks; ++x) {
+        for (int x = 0; x < kMine; ++x) {
             const int k = lane + 64 * x, r = k / vtile::kChunks, c = (k % vtile::kChunks) * vtile::kPer;
             const u32x4 zero = {0u, 0u, 0u, 0u};
             vv[x] = r < keys && c < p.width ? *reinterpret_cast<const u32x4 *>(vbase + (int64_t)(key0 + r) * p.v_stride + c) : zero;
         }
-        // distances of the step's keys from the query rows: from the last key to the first
-        const int from = u.first - (step + kSplitStep - 1), met = kSplitStep + u.nq - 1;
         if (step > begin) __syncthreads();
         bool hides = false;
-        for (int x = threadIdx.x; x < met * p.group; x += kAttnThreads) {
-            const int d = from + x / p.group, h = x % p.group, c = d < low ? low : d > high ? high : d;
-            float b = 0.f;
-            if (p.bias) {
-                const int k = p.bucket_of[c - low];
-                if (k < 0 || k >= p.buckets) atomicOr(p.flags, kFlagRowRange);
-                else b = p.bias[(int64_t)k * p.heads + kvh * p.group + h] * kLog2e;
+        if ((int)threadIdx.x < met) {                      // a thread each: kSplitStep + 15 of them at most
+            const bool none = bucket < 0 || bucket >= p.buckets;
+            if (p.bias && none) atomicOr(p.flags, kFlagRowRange);
+            for (int h = 0; h < p.group; ++h) {
+                const float b = none ? 0.f : p.bias[(int64_t)bucket * p.heads + kvh * p.group + h] * kLog2e;
+                bias_lds[threadIdx.x * p.group + h] = b;
+                hides |= b == neg_inf();
             }
-            bias_lds[x] = b;
-            hides |= b == neg_inf();
         }
         hides = __syncthreads_or(hides) != 0;
         if (keys > 0) {
             const bool edge = hides || (p.causal && key0 + keys - 1 > u.first);
             bool odd = false;
 #pragma unroll
-            for (int x = 0; x < vtile::kChunks; ++x) {
+            for (int x = 0; x < kMine; ++x) {
                 if (edge) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) vv[x][i] = clean_word<T>(vv[x][i], odd);
@@ -341,19 +351,24 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_split_
             }
             odd = __any(odd) != 0;
             wave_lds_order();
-            f32x4 s[4];
+            f32x4 s[kSplitKeys / 16];
             float top = neg_inf();
-            const int seen = p.causal && pos + 1 < stop ? pos + 1 : stop;
+            const int seen = !live ? 0 : p.causal && pos + 1 < stop ? pos + 1 : stop;
             const float *b = bias_lds + ((pos - key0) - from) * p.group + head - kvh * p.group;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < kSplitKeys / 16; ++k) {
                 s[k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < KC; ++c) mma(s[k], kf[k][c], qf[c]);
+            }
+            settle();
+#pragma unroll
+            for (int k = 0; k < kSplitKeys / 16; ++k) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int key = 16 * k + 4 * g + r;
-                    s[k][r] = live && key0 + key < seen ? s[k][r] * scale2 + b[-key * p.group] : neg_inf();
+                    const float x = s[k][r] * scale2 + b[-key * p.group];      // in the strip for every key of the step
+                    s[k][r] = key0 + key < seen ? x : neg_inf();
                     top = fmaxf(top, s[k][r]);
                 }
             }
@@ -366,14 +381,14 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_split_
 #pragma unroll
                 for (int r = 0; r < 4; ++r) acc[d][r] *= shrink;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < kSplitKeys / 16; ++k)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     s[k][r] = __builtin_amdgcn_exp2f(s[k][r] - base);
                     l += s[k][r];
                 }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < kSplitKeys / 32; ++c) {
                 piece<T> pf;
                 as_operand(pf, s[2 * c], s[2 * c + 1]);
 #pragma unroll
@@ -386,7 +401,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_split_
             settle();
             if (odd) {                                  // the values left out of the product, for the rows that see them
                 for (int k = 0; k < keys; ++k) {
-                    const bool sees = live && key0 + k < seen && b[-k * p.group] != neg_inf();
+                    const bool sees = key0 + k < seen && b[-k * p.group] != neg_inf();
 #pragma unroll
                     for (int d = 0; d < MT; ++d)
 #pragma unroll
@@ -466,7 +481,7 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(attn_params p) 
     if (qa < 0 || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv || at_row < qa || at_row >= qb || qb - qa > max_q ||
         kb - ka > 0x3fffffff)
         return;
-    const int nk = rows_in_use(p.kv_lengths, b, (int)(kb - ka));
+    const int nk = rows_in_use(p.kv_lengths ? p.kv_lengths[b] : kb - ka, (int)(kb - ka));
     const int chunk = 1 << shift;
     if (nk <= chunk) return;                            // written by the workgroup that had them all
     const int row = (int)(at_row - qa);
@@ -479,16 +494,26 @@ __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(attn_params p) 
 #pragma unroll
     for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
     const float base = top == neg_inf() ? 0.f : top;
-    constexpr int kMine = DH < kWave ? 1 : DH / kWave;
+    constexpr int kMine = DH < kWave ? 1 : DH / kWave, kAtOnce = 8;
     float o[kMine] = {}, sum = 0.f;
-    for (int c = 0; c < chunks; ++c) {
-        const int64_t at = first + c * apart;
-        const float part = __builtin_amdgcn_exp2f(p.split_ml[2 * at] - base);
-        sum += part * p.split_ml[2 * at + 1];
+    for (int c0 = 0; c0 < chunks; c0 += kAtOnce) {          // eight chunks asked for before the first is used
+        float part[kAtOnce], l[kAtOnce], a[kAtOnce][kMine];
 #pragma unroll
-        for (int x = 0; x < kMine; ++x) {
-            const int col = lane + 64 * x;
-            if (col < DH) o[x] += part * p.split_acc[at * DH + col];
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int64_t at = first + min(c0 + i, chunks - 1) * apart;
+            part[i] = p.split_ml[2 * at];
+            l[i] = p.split_ml[2 * at + 1];
+#pragma unroll
+            for (int x = 0; x < kMine; ++x) a[i][x] = p.split_acc[at * DH + min(lane + 64 * x, DH - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+            if (c0 + i < chunks) {
+                const float weight = __builtin_amdgcn_exp2f(part[i] - base);
+                sum += weight * l[i];
+#pragma unroll
+                for (int x = 0; x < kMine; ++x) o[x] += weight * a[i][x];
+            }
         }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
@@ -638,7 +663,7 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
         if (split) {
             p.split_acc = static_cast<float *>(a.work);
             p.split_ml = p.split_acc + split_rows(a) * DH;
-            const size_t lds = kAttnWaves * sizeof(tile<T, DH>) + (size_t)(kSplitStep + a.max_q) * p.group * sizeof(float);
+            const size_t lds = split_rows_lds<T, DH> + (size_t)(kSplitStep + a.max_q) * p.group * sizeof(float);
             const int done = launch_attention(ctx, attn_split_kernel<T, DH>, attn_slots(a.n_kv, a.batch, p.split_shift) * a.kv_heads,
                                               lds, s, "attn_split", p);
             if (done != FS_OK || a.n_kv <= 1ll << p.split_shift) return done;     // nobody has several chunks

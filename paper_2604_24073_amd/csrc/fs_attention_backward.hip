@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int head = blockIdx.x % p.heads;
     const int slot = (int)(blockIdx.x / p.heads);
-    if (head == 0) check_layout(p, slot);
+    if (head == 0) check_layout(p, slot, (int)(gridDim.x / p.heads));
     user u;
     int index;
     float *part = p.dbias ? p.bias_part + ((int64_t)slot * p.heads + head) * p.buckets : nullptr;
