@@ -163,6 +163,9 @@ struct window {
     __device__ __forceinline__ u32x4 load(int offset) const {
         return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, offset, 0, 0));
     }
+    __device__ __forceinline__ float load1(int offset) const {
+        return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, offset, 0, 0));
+    }
 };
 
 // A thread's chunks of the next tile on their way from memory to LDS.
@@ -379,11 +382,9 @@ struct strip {
     static __host__ __device__ int entries(int distances, bool causal) {
         return (causal ? distances : 2 * distances - 1) + 2 * kPad;
     }
-    // the bucket of a distance, -1 where it is none
-    __device__ __forceinline__ int bucket(const attn_params &p, int d) const {
-        const int k = p.bucket_of[min(max(d, low), high) - low];
-        return k < p.buckets ? max(k, -1) : -1;
-    }
+    // what the table has for a distance, and the bucket that is: -1 where it is none
+    __device__ __forceinline__ int entry(const attn_params &p, int d) const { return p.bucket_of[min(max(d, low), high) - low]; }
+    static __device__ __forceinline__ int bucket(const attn_params &p, int k) { return k < p.buckets ? max(k, -1) : -1; }
     // Distances from `from` to `to` (and kPad around) are met.  Returns whether any bias of them hides (is -inf); has a barrier.
     __device__ __forceinline__ bool fill(const attn_params &p, int head, float *lds, int from, int to) {
         at = lds;
@@ -395,7 +396,7 @@ struct strip {
         for (int d = a + (int)threadIdx.x; d <= b; d += kAttnThreads) {
             float x = 0.f;
             if (p.bias) {
-                const int k = bucket(p, d);
+                const int k = bucket(p, entry(p, d));
                 if (k < 0) atomicOr(p.flags, kFlagRowRange);
                 else x = p.bias[(int64_t)k * p.heads + head] * kLog2e;
             }

@@ -245,13 +245,13 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             // of a tile beyond the table, the distances nearest to it have the same bias
             const int near = min(max(nearest, bias.low - (62 + 16 * QT)), bias.high);
             const float *bb = bias.at + bias.zero + near + (j - 4 * g) + 12;
-            // the buckets of the distances, on their way while the scores are made
+            // the table's entries for the distances, on their way while the scores are made (and not looked at before)
             int buckets[QT][2];
             if (part) {
 #pragma unroll
                 for (int t = 0; t < QT; ++t) {
-                    buckets[t][0] = bias.bucket(p, near + 16 * t + lane);
-                    buckets[t][1] = bias.bucket(p, near + 16 * t + min(64 + lane, kSpan - 1));
+                    buckets[t][0] = bias.entry(p, near + 16 * t + lane);
+                    buckets[t][1] = bias.entry(p, near + 16 * t + min(64 + lane, kSpan - 1));
                 }
             }
             // element r of s[t][k]: query row wrow + 16 t + j, key key0 + 16 k + 4 g + r
@@ -318,10 +318,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                     for (int t = 0; t < QT; ++t)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) share += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
-                    sums.one(__builtin_amdgcn_readfirstlane(buckets[0][0]), share);
+                    sums.one(__builtin_amdgcn_readfirstlane(bias.bucket(p, buckets[0][0])), share);
                 } else {
 #pragma unroll
-                    for (int t = QT - 1; t >= 0; --t) add_by_bucket(sums, skew + w * kSkew, s[t], buckets[t][0], buckets[t][1]);
+                    for (int t = QT - 1; t >= 0; --t) add_by_bucket(sums, skew + w * kSkew, s[t], bias.bucket(p, buckets[t][0]), bias.bucket(p, buckets[t][1]));
                 }
             }
         }
@@ -397,29 +397,40 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
     qr.place(p.q_stride, p.width);
     dr.place(orow, p.width);
     float stat = 0.f;
-    const auto fetch = [&](int n) {
-        const int head = kvh * p.group + n / tiles, r0 = from + (n % tiles) * kTile;
-        qr.load(static_cast<const T *>(p.q) + (u.q0 + r0) * p.q_stride + head * p.width, p.q_stride, u.nq - r0);
-        dr.load(static_cast<const T *>(p.dout) + (u.q0 + r0) * orow + head * p.width, orow, u.nq - r0);
-        if (threadIdx.x < 2 * kTile) {
-            const int r = r0 + (threadIdx.x & (kTile - 1));
-            const bool lse = threadIdx.x < kTile;
-            stat = lse ? neg_inf() : 0.f;                                         // rows that see nothing and rows that are none
-            if (r < u.nq) {
-                const float x = (lse ? p.lse : p.delta)[(int64_t)head * p.n_q + u.q0 + r];
-                if (!lse) stat = -x;
-                else if (x != neg_inf()) stat = -x * inv_scale;
-            }
+    // The tile that is fetched next: its first row among the user's, its head, and where its rows begin.
+    int next_row = from, next_head = kvh * p.group;
+    const T *next_q, *next_o;
+    const float *next_stat;                   // of wavefront 0: lse, of wavefront 1: D
+    const auto begin_head = [&]() {
+        next_row = from;
+        next_q = static_cast<const T *>(p.q) + (u.q0 + from) * p.q_stride + next_head * p.width;
+        next_o = static_cast<const T *>(p.dout) + (u.q0 + from) * orow + next_head * p.width;
+        next_stat = (w == 0 ? p.lse : p.delta) + (int64_t)next_head * p.n_q + u.q0 + from;
+    };
+    const auto fetch = [&]() {
+        const int rows = min(u.nq - next_row, kTile);
+        qr.load(next_q, p.q_stride, rows);
+        dr.load(next_o, orow, rows);
+        // a row's lse or D, as it is: whatever is made of it here would wait for it here
+        if (w < 2) stat = window(next_stat, 4 * rows).load1(4 * lane);
+    };
+    const auto advance = [&]() {
+        next_row += kTile;
+        next_q += kTile * p.q_stride;
+        next_o += kTile * orow;
+        next_stat += kTile;
+        if (next_row >= u.nq) {
+            ++next_head;
+            begin_head();
         }
     };
     strip<kPad> bias;
     bool hides = false;
     // some of the tile's rows do not see all keys of the workgroup, or some of either are none
-    const auto edge = [&](int n) {
-        const int r0 = from + (n % tiles) * kTile;
+    const auto edge = [&](int r0) {
         return key_first + kKeys > u.nk || r0 + kTile > u.nq || (p.causal && u.first + r0 < key_first + kKeys - 1);
     };
-    const auto stage = [&](int n, bool clean) {
+    const auto stage = [&](int n, int r0, bool clean) {
         const int b = n & 1;
         if (kBufs == 1) __syncthreads();
         if (clean) {
@@ -429,22 +440,29 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
         }
         qr.store(qt[n & (kBufs - 1)]);
         dr.store(ot[n & (kBufs - 1)]);
-        if (threadIdx.x < 2 * kTile) stats[2 * b * kTile + threadIdx.x] = stat;
+        if (w < 2) {
+            const bool lse = w == 0, row = r0 + lane < u.nq;
+            const float less = lse ? (stat == neg_inf() ? neg_inf() : -stat * inv_scale) : -stat;
+            // rows that see nothing and rows that are none
+            stats[2 * b * kTile + threadIdx.x] = row ? less : lse ? neg_inf() : 0.f;
+        }
     };
-    const auto fill = [&](int n) {
-        return bias.fill(p, kvh * p.group + n / tiles, bias_lds, u.first + from - (key_first + kKeys - 1), u.first + u.nq - 1 - key_first);
+    const auto fill = [&](int head) {
+        return bias.fill(p, head, bias_lds, u.first + from - (key_first + kKeys - 1), u.first + u.nq - 1 - key_first);
     };
     bool masked = false;                      // the tile at hand was cleaned, and is worked on with its marks and masks
     if (turns > 0) {
-        fetch(0);
-        hides = fill(0);
-        stage(0, masked = edge(0) || hides);
+        begin_head();
+        fetch();
+        hides = fill(next_head);
+        stage(0, from, masked = edge(from) || hides);
     }
     for (int n = 0; n < turns; ++n) {
         __syncthreads();
-        if (n > 0 && n % tiles == 0) hides = fill(n);
-        const int b = n & 1, r0 = from + (n % tiles) * kTile, pos0 = u.first + r0, head = kvh * p.group + n / tiles;
-        if (n + 1 < turns) fetch(n + 1);
+        const int b = n & 1, r0 = next_row, pos0 = u.first + r0, head = next_head;
+        if (r0 == from && n > 0) hides = fill(head);
+        advance();
+        if (n + 1 < turns) fetch();
         const tile<T, DH> &Q = qt[n & (kBufs - 1)], &O = ot[n & (kBufs - 1)];
         // A tile has one form from its first product to its last, so that the products of one half run beside the powers of the
         // other: mask - some pairs are not seen, or are none; away - all distances are beyond the table.
@@ -556,8 +574,8 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
         }
         if (n + 1 < turns) {
             // a head's first tile is put down before its bias is known to hide nothing
-            masked = edge(n + 1) || hides || (n + 1) % tiles == 0;
-            stage(n + 1, masked);
+            masked = edge(next_row) || hides || next_row == from;
+            stage(n + 1, next_row, masked);
         }
     }
 #pragma unroll
