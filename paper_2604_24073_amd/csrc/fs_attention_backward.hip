@@ -18,13 +18,25 @@ struct bucket_sums {
     float run = 0.f;        // a lane's share of the bucket below, not yet in its bin
     int now = -1;
 
-    static __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-        for (int m = 1; m < kWave; m <<= 1) x += __shfl_xor(x, m, kWave);
-        return x;
+    // a neighbour's value, without a trip through LDS: CTRL is one of the vector units' lane patterns
+    template <int CTRL, int ROWS = 0xf>
+    static __device__ __forceinline__ float from(float x) {
+        return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), CTRL, ROWS, 0xf, false));
+    }
+    static __device__ __forceinline__ float wave_sum(float x) {          // in every lane
+        x += from<0x128>(x);                                             // row_ror: 8, 4, 2, 1
+        x += from<0x124>(x);
+        x += from<0x122>(x);
+        x += from<0x121>(x);
+        return column_sum(x);
+    }
+    // A single lane's addition to a bin of its wavefront's own: nothing else is added to it at the same time, and LDS keeps a
+    // wavefront's order, so this is an addition that nobody waits for, not one whose order is open.
+    __device__ __forceinline__ void put(int bucket, float x) {
+        __hip_atomic_fetch_add(bins + bucket, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     }
     __device__ __forceinline__ void add(int bucket, float total) {       // of the whole wavefront
-        if (bucket >= 0 && (threadIdx.x & 63) == 0) bins[bucket] += total;
+        if (bucket >= 0 && (threadIdx.x & 63) == 0) put(bucket, total);
     }
     __device__ __forceinline__ void flush() {
         add(now, wave_sum(run));
@@ -55,22 +67,22 @@ struct bucket_sums {
             }
             return;
         }
-        const int start = 63 - __clzll((long long)(heads & (~0ull >> (63 - lane))));
-        const int in_row = lane & 15;
-        float x = value;
-#pragma unroll
-        for (int d = 1; d < 16; d <<= 1) {
-            const float y = __uint_as_float(__builtin_amdgcn_ds_bpermute(4 * (lane - d), (int)__float_as_uint(x)));
-            x += in_row >= d && lane - d >= start ? y : 0.f;
-        }
-        {
-            const float y = __uint_as_float(__builtin_amdgcn_ds_bpermute(4 * ((lane & 32) + 15), (int)__float_as_uint(x)));
-            x += (lane & 16) && (lane & 32) + 15 >= start ? y : 0.f;
-            const float z = __uint_as_float(__builtin_amdgcn_ds_bpermute(4 * 31, (int)__float_as_uint(x)));
-            x += (lane & 32) && 31 >= start ? z : 0.f;
-        }
+        const int start = 63 - __clzll((long long)(heads & (~0ull >> (63 - lane)))), in_row = lane & 15;
+        float x = value, y;
+        y = from<0x111>(x);                                              // row_shr: 1, 2, 4, 8
+        x += in_row >= 1 && lane - 1 >= start ? y : 0.f;
+        y = from<0x112>(x);
+        x += in_row >= 2 && lane - 2 >= start ? y : 0.f;
+        y = from<0x114>(x);
+        x += in_row >= 4 && lane - 4 >= start ? y : 0.f;
+        y = from<0x118>(x);
+        x += in_row >= 8 && lane - 8 >= start ? y : 0.f;
+        y = from<0x142, 0xa>(x);                                         // a row's last lane to the next row: rows 1 and 3
+        x += (lane & 16) && (lane & 32) + 15 >= start ? y : 0.f;
+        y = from<0x143, 0xc>(x);                                         // a half's last lane to the other half
+        x += (lane & 32) && 31 >= start ? y : 0.f;
         const bool last = lane == 63 || ((heads >> 1) >> lane & 1);
-        if (last && bucket >= 0) bins[bucket] += x;
+        if (last && bucket >= 0) put(bucket, x);                         // a bucket each
     }
 };
 
@@ -118,8 +130,15 @@ __device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, co
         sums.each(b1, lane < 15 ? far : 0.f);
         return;
     }
-    // the distances from `at` on have another bucket than those before (none of them where nothing changes)
-    const int at = h0 ? 63 - __clzll((long long)h0) : h1 ? 127 - __clzll((long long)h1) : kSpan;
+    if (changes == 0) {
+        float all = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) all += (s[k][0] + s[k][1]) + (s[k][2] + s[k][3]);
+        sums.one(__builtin_amdgcn_readfirstlane(b0), all);
+        return;
+    }
+    // the distances from `at` on have another bucket than those before
+    const int at = h0 ? 63 - __clzll((long long)h0) : 127 - __clzll((long long)h1);
     const int mine = j + 63 - 4 * g;                       // element r of s[k] has distance mine - 16 k - r
     float near = 0.f, far = 0.f;
 #pragma unroll
@@ -130,7 +149,7 @@ __device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, co
             far += beyond ? s[k][r] : 0.f;
             near += beyond ? 0.f : s[k][r];
         }
-    if (changes) sums.one(__builtin_amdgcn_readlane(b1, 14), far);
+    sums.one(__builtin_amdgcn_readlane(b1, 14), far);
     sums.one(__builtin_amdgcn_readfirstlane(b0), near);
 }
 
