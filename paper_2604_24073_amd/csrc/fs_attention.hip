@@ -36,6 +36,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
     user u;
     int index;
     if (!find_user(p, p.q_offsets, slot, kShift, u, index) || (int64_t)index * kRows >= u.nq) return;
+    index = (u.nq - 1) / kRows - index;                              // the last rows, which see most, begin first
     const int row0 = index * kRows;                                  // first query row of the workgroup
     const int rows = u.nq - row0 < kRows ? u.nq - row0 : kRows;
     const int pos0 = u.first + row0, pos_last = pos0 + rows - 1;

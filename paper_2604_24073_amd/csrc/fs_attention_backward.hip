@@ -180,6 +180,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             for (int b = threadIdx.x; b < p.buckets; b += kAttnThreads) part[b] = 0.f;
         return;
     }
+    index = (u.nq - 1) / kRows - index;                                           // the last rows, which see most, begin first
     const int row0 = index * kRows;
     const int rows = u.nq - row0 < kRows ? u.nq - row0 : kRows;
     const int pos0 = u.first + row0, pos_last = pos0 + rows - 1;
