@@ -86,71 +86,92 @@ struct bucket_sums {
     }
 };
 
-// A wavefront's 16 query rows x 64 keys, summed along its diagonals: value (q, key) belongs to distance q - key + 63 of the
-// 79.  Each value is written where its distance's row has column q; a row then has at most 16, and rows d and d + 64 share
-// them: row d has columns up to d, row d + 64 those behind.
+// Sixteen query rows x 64 keys, summed along their diagonals: value (q, key) belongs to distance q - key + 63 of the 79.
+// Each is written where its distance's row has column q, and a lane adds up a row.  A row's sixteen columns are four pieces of
+// 16 bytes, at places that turn with the row, so that sixteen lanes read their rows' pieces from different banks.  The columns
+// that a row has no value for are zeros from the start (clear_skew) and never written.
 constexpr int kSpan = kTile + 15;
-constexpr int kSkewLd = 17;
-constexpr int kSkew = kSpan * kSkewLd;
+constexpr int kSkew = kSpan * 16;
+__device__ __forceinline__ void clear_skew(float *skew) {
+    for (int i = threadIdx.x & 63; i < kSkew; i += kWave) skew[i] = 0.f;
+}
+__device__ __forceinline__ float row_total(const float *skew, int row) {
+    const float *at = skew + 16 * row;
+    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(at + 4 * (c ^ ((row >> 2) & 3)));
+        sum += (x[0] + x[1]) + (x[2] + x[3]);
+    }
+    return sum;
+}
+// near: the sum of distance `lane`; far: of distance 64 + lane, where there is one
 __device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], float &near, float &far) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+    for (int r = 0; r < 4; ++r) {
+        const int d = j + 63 - 4 * g - r;                  // of key 4 g + r; sixteen keys further on the places turn alike
+        float *at = skew + 16 * d + 4 * ((j >> 2) ^ ((d >> 2) & 3)) + (j & 3);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) skew[(j + 63 - 16 * k - 4 * g - r) * kSkewLd + j] = s[k][r];
-    wave_lds_order();
-    near = far = 0.f;
-    const float *row = skew + lane * kSkewLd;
-    const int cut = lane < 15 ? lane : 15;
-#pragma unroll
-    for (int q = 0; q < 16; ++q) {
-        const float x = row[q + (q > cut ? 64 * kSkewLd : 0)];
-        near += q <= cut ? x : 0.f;
-        far += q <= cut ? 0.f : x;
+        for (int k = 0; k < 4; ++k) at[-256 * k] = s[k][r];
     }
+    wave_lds_order();
+    near = row_total(skew, lane);
+    far = lane < 15 ? row_total(skew, 64 + lane) : 0.f;
     wave_lds_order();
 }
 
-// The 16 x 64 values s of a wavefront added to the sums of their buckets; b0: the bucket of the lane's of the first 64 distances,
-// b1: of the 15 behind them, the last one's in the lanes that have none.
-// Tables of distances have few buckets in 79 distances but near zero: one bucket takes every lane's sum as it is, two
-// are told apart by comparing distances, and only more are brought into the order of the distances.  Further distances come
-// first: the tiles go from far to near, and a bucket's lanes are added up when the next bucket begins.
-__device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, const f32x4 (&s)[4], int b0, int b1) {
+// The 16 QT x 64 values s of a wavefront added to the sums of their buckets; b0: the bucket of the lane's of the first 64
+// distances, b1: of those behind them, the last one's in the lanes that have none.  Tables of distances have few buckets in so
+// many distances but near zero: one bucket takes every lane's sum as it is, two are told apart by comparing distances, and only
+// more are brought into the order of the distances.  Further distances come first: the tiles go from far to near, and a
+// bucket's lanes are added up when the next bucket begins.
+template <int QT>
+__device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, const f32x4 (&s)[QT][4], int b0, int b1) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
     const int last0 = __builtin_amdgcn_readlane(b0, 63), before0 = __builtin_amdgcn_update_dpp(b0, b0, 0x138, 0xf, 0xf, false);
     int before1 = __builtin_amdgcn_update_dpp(b1, b1, 0x138, 0xf, 0xf, false);
     before1 = lane == 0 ? last0 : before1;
-    uint64_t h0 = __ballot(b0 != before0), h1 = __ballot(b1 != before1);          // where a bucket begins
+    const uint64_t h0 = __ballot(b0 != before0), h1 = __ballot(b1 != before1);    // where a bucket begins
     const int changes = __popcll(h0) + __popcll(h1);
-    if (changes > 1) {
-        float near, far;
-        diagonal_sums(skew, s, near, far);
-        sums.each(b0, near);
-        sums.each(b1, lane < 15 ? far : 0.f);
-        return;
-    }
     if (changes == 0) {
         float all = 0.f;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) all += (s[k][0] + s[k][1]) + (s[k][2] + s[k][3]);
+        for (int t = 0; t < QT; ++t)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) all += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
         sums.one(__builtin_amdgcn_readfirstlane(b0), all);
-        return;
-    }
-    // the distances from `at` on have another bucket than those before
-    const int at = h0 ? 63 - __clzll((long long)h0) : 127 - __clzll((long long)h1);
-    const int mine = j + 63 - 4 * g;                       // element r of s[k] has distance mine - 16 k - r
-    float near = 0.f, far = 0.f;
+    } else if (changes == 1) {
+        // the distances from `at` on have another bucket than those before
+        const int at = h0 ? 63 - __clzll((long long)h0) : 127 - __clzll((long long)h1);
+        const int mine = j + 63 - 4 * g;                   // element r of s[t][k] has distance mine + 16 t - 16 k - r
+        float near = 0.f, far = 0.f;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
+        for (int t = 0; t < QT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const bool beyond = mine >= at + 16 * k + r;
-            far += beyond ? s[k][r] : 0.f;
-            near += beyond ? 0.f : s[k][r];
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const bool beyond = mine >= at + 16 * k + r - 16 * t;
+                    far += beyond ? s[t][k][r] : 0.f;
+                    near += beyond ? 0.f : s[t][k][r];
+                }
+        sums.one(__builtin_amdgcn_readlane(b1, 63), far);    // the last distance's
+        sums.one(__builtin_amdgcn_readfirstlane(b0), near);
+    } else {
+        float near, far;
+        diagonal_sums(skew, s[0], near, far);
+        if constexpr (QT == 2) {
+            // the second sixteen rows' distances are sixteen further on
+            float near2, far2;
+            diagonal_sums(skew, s[1], near2, far2);
+            const float y = __shfl(near2, (lane + 48) & 63, kWave), z = __shfl(far2, (lane + 48) & 63, kWave);
+            near += lane >= 16 ? y : 0.f;
+            far += lane < 16 ? y : z;                      // z: zeros from distance 95 on
         }
-    sums.one(__builtin_amdgcn_readlane(b1, 14), far);
-    sums.one(__builtin_amdgcn_readfirstlane(b0), near);
+        sums.each(b0, near);
+        sums.each(b1, far);
+    }
 }
 
 // ---- query rows ---------------------------------------------------------------------------------------------------------------
@@ -233,8 +254,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
     strip<kPad> bias;
     bucket_sums sums;
     sums.bins = bins + w * p.buckets;
-    if (part)
+    if (part) {
         for (int b = lane; b < p.buckets; b += kWave) sums.bins[b] = 0.f;
+        clear_skew(skew + w * kSkew);
+    }
     const bool hides = bias.fill(p, head, bias_lds, pos0 - (end > 0 ? end - 1 : 0), pos_last);
     const float scale2 = p.scale * kLog2e;
 
@@ -266,13 +289,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             const int near = min(max(nearest, bias.low - (62 + 16 * QT)), bias.high);
             const float *bb = bias.at + bias.zero + near + (j - 4 * g) + 12;
             // the table's entries for the distances, on their way while the scores are made (and not looked at before)
-            int buckets[QT][2];
+            int buckets[2];
             if (part) {
-#pragma unroll
-                for (int t = 0; t < QT; ++t) {
-                    buckets[t][0] = bias.entry(p, near + 16 * t + lane);
-                    buckets[t][1] = bias.entry(p, near + 16 * t + min(64 + lane, kSpan - 1));
-                }
+                buckets[0] = bias.entry(p, near + lane);
+                buckets[1] = bias.entry(p, near + min(64 + lane, 62 + 16 * QT));
             }
             // element r of s[t][k]: query row wrow + 16 t + j, key key0 + 16 k + 4 g + r
             f32x4 s[QT][4];
@@ -338,10 +358,9 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                     for (int t = 0; t < QT; ++t)
 #pragma unroll
                         for (int k = 0; k < 4; ++k) share += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
-                    sums.one(__builtin_amdgcn_readfirstlane(bias.bucket(p, buckets[0][0])), share);
+                    sums.one(__builtin_amdgcn_readfirstlane(bias.bucket(p, buckets[0])), share);
                 } else {
-#pragma unroll
-                    for (int t = QT - 1; t >= 0; --t) add_by_bucket(sums, skew + w * kSkew, s[t], bias.bucket(p, buckets[t][0]), bias.bucket(p, buckets[t][1]));
+                    add_by_bucket<QT>(sums, skew + w * kSkew, s, bias.bucket(p, buckets[0]), bias.bucket(p, buckets[1]));
                 }
             }
         }

@@ -111,6 +111,17 @@ def test_bias_tables(ctx, dtype, causal, buckets, distances):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("run", [17, 50, 134])
+def test_buckets_that_begin_anywhere_in_a_tile(ctx, dtype, causal, run):
+    """Runs of distances that share a bucket: none, one or several begin in a tile, at every place in it."""
+    for shift in range(0, run, run // 8):
+        c = Case([650, 130], heads=1, kv_heads=1, width=32, dtype=dtype, causal=causal, buckets=100, distances=600, seed=shift)
+        c.bucket_of = ((torch.arange(c.bucket_of.shape[0]) + shift) // run).to(torch.int32)
+        c.check(ctx)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_widest_with_the_largest_tables(ctx, dtype):
     for causal in (True, False):
         Case([150, 65], width=128, heads=2, kv_heads=1, buckets=1024, distances=4096, dtype=dtype, causal=causal).check(ctx)
