@@ -407,6 +407,12 @@ struct strip {
     }
 };
 
+// Whether the sums of a row's scores begin at what the scores are less by, -lse / scale, which saves an addition for every score.
+// A matrix product keeps 24 bits of its running sum, which are then spent on the size of lse / scale: enough where the factors
+// have 8 bits, not where they have 24.
+template <typename T>
+constexpr bool from_less = sizeof(T) == 2;
+
 // Wavefronts of a SIMD that a kernel is compiled for.  With two or more of them asked for, all of a wavefront's registers can be
 // named by every instruction, and the accumulators stay where the vector units can read them.
 template <typename T, int DH>

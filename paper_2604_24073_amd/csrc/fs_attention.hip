@@ -67,7 +67,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 
     // the product with P's second term has a sum of its own: an infinity among the values meets a zero or a negative rest there
     f32x4 acc[QT][MT] = {}, acc_rest[EXACT ? QT : 1][MT] = {};
-    // m: what the row's scores are less by, where their sums begin (as less, in the product's own terms); it follows the row's
+    // m: what the row's scores are less by (less: the same in the product's own terms); it follows the row's
     // maximum once that is 2^8 ahead, which is enough to keep the powers in range, and at once from the first key seen on
     float m[QT], l[QT], less[QT], ahead[QT];
     const float inv_scale2 = 1.f / scale2;
@@ -101,7 +101,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
 #pragma unroll
-                for (int t = 0; t < QT; ++t) s[t][k] = f32x4{less[t], less[t], less[t], less[t]};
+                for (int t = 0; t < QT; ++t) {
+                    const float at = from_less<T> ? less[t] : 0.f;
+                    s[t][k] = f32x4{at, at, at, at};
+                }
 #pragma unroll
                 for (int c = 0; c < KC; ++c) {
                     piece<T> a;
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[t][k][r] = s[t][k][r] * scale2 + b;
+                        for (int r = 0; r < 4; ++r) s[t][k][r] = s[t][k][r] * scale2 + (from_less<T> ? b : b - m[t]);
             } else {
                 const float *b = bias.at + bias.zero + nearest + (j - 4 * g) + 12;
 #pragma unroll
@@ -127,7 +130,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) s[t][k][r] = s[t][k][r] * scale2 + b[51 + 16 * t - 16 * k - r];
+                        for (int r = 0; r < 4; ++r) {
+                            const float x = b[51 + 16 * t - 16 * k - r];
+                            s[t][k][r] = s[t][k][r] * scale2 + (from_less<T> ? x : x - m[t]);
+                        }
             }
             if ((p.causal && key0 + kTile - 1 > wpos) || key0 + kTile > u.nk) {
 #pragma unroll

@@ -218,8 +218,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
 
     const int wrow = row0 + 16 * QT * w, wpos = u.first + wrow;
     piece<T> qf[QT][KC], of[QT][KC];
-    // what a row's scores and dO V^T are less by is where their sums begin: -lse / scale, -delta
-    float less_s[QT], less_dp[QT];
+    // What a row's scores are less by, as from_less has it, and its D.  D is taken from a finished dO V^T: a sum that began at -D
+    // would be cut off at D's size, always downwards, and the bias's gradient adds up millions of them (16384 rows: 7e-6 of it
+    // off in place of 1e-6).
+    float less_s[QT], delta[QT];
     const int64_t orow = p.heads * (int64_t)p.width;                              // out and dout are packed
     const int64_t obase = u.q0 * orow + head * p.width;
 #pragma unroll
@@ -242,12 +244,12 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             for (int i = 0; i < 8; ++i) sum += o[i] * d[i];
         }
         sum = column_sum(sum);
-        less_dp[t] = -sum;
+        delta[t] = sum;
         less_s[t] = neg_inf();                                                    // a row that sees nothing: P = 0
         if (live) {
             const int64_t at = (int64_t)head * p.n_q + u.q0 + row;
             const float x = p.lse[at];
-            if (x != neg_inf()) less_s[t] = -x / p.scale;
+            if (x != neg_inf()) less_s[t] = from_less<T> ? -x / p.scale : -x * kLog2e;
             if (g == 0) p.delta[at] = sum;
         }
     }
@@ -301,11 +303,11 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             const auto work = [&](auto mask, auto away) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    f32x4 dp[QT];
+                    f32x4 dp[QT] = {};
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
-                        s[t][k] = f32x4{less_s[t], less_s[t], less_s[t], less_s[t]};
-                        dp[t] = f32x4{less_dp[t], less_dp[t], less_dp[t], less_dp[t]};
+                        const float at = from_less<T> ? less_s[t] : 0.f;
+                        s[t][k] = f32x4{at, at, at, at};
                     }
 #pragma unroll
                     for (int c = 0; c < KC; ++c) {
@@ -325,7 +327,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float b = away() ? far : bb[51 + 16 * t - 16 * k - r];
-                            float power = s[t][k][r] * scale2 + b, d = dp[t][r];
+                            float power = s[t][k][r] * scale2 + (from_less<T> ? b : b + less_s[t]), d = dp[t][r] - delta[t];
                             if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen ? power + x[r] : neg_inf();
                             const float e = __builtin_amdgcn_exp2f(power);
                             if constexpr (mask()) d = e == 0.f ? 0.f : d;
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
     extern __shared__ __align__(16) char lds[];
     constexpr int kBufs = tile_buffers<T, DH>;
     tile<T, DH> *qt = reinterpret_cast<tile<T, DH> *>(lds), *ot = qt + kBufs;
-    float *stats = reinterpret_cast<float *>(ot + kBufs);                         // [2][-lse / scale, -delta][kTile]
+    float *stats = reinterpret_cast<float *>(ot + kBufs);                         // [2][what scores are less by, -D][kTile]
     float *mark = stats + 4 * kTile;                                              // [2][q, dout][kTile]
     uint32_t *odd = reinterpret_cast<uint32_t *>(mark + 4 * kTile);               // [2][wavefronts]
     float *bias_lds = reinterpret_cast<float *>(odd + 2 * kAttnWaves);
@@ -481,7 +483,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
         dr.store(ot[n & (kBufs - 1)]);
         if (w < 2) {
             const bool lse = w == 0, row = r0 + lane < u.nq;
-            const float less = lse ? (stat == neg_inf() ? neg_inf() : -stat * inv_scale) : -stat;
+            const float less = lse ? (stat == neg_inf() ? neg_inf() : -stat * (from_less<T> ? inv_scale : kLog2e)) : -stat;
             // rows that see nothing and rows that are none
             stats[2 * b * kTile + threadIdx.x] = row ? less : lse ? neg_inf() : 0.f;
         }
@@ -517,14 +519,14 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
                 const float *bb = bias.at + bias.zero + near + (4 * g - j + 15);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    // what a row's scores and dO V^T are less by is where their sums begin
+                    // dO V^T less D goes only into a product of such factors: it begins where the scores do, at -D
                     const int at = 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
                     const f32x4 less_s = *reinterpret_cast<const f32x4 *>(stats + at);
                     const f32x4 less_dp = *reinterpret_cast<const f32x4 *>(stats + kTile + at);
 #pragma unroll
                     for (int t = 0; t < KT; ++t) {
-                        s[h][t] = less_s;
-                        dp[h][t] = less_dp;
+                        s[h][t] = from_less<T> ? less_s : f32x4{0.f, 0.f, 0.f, 0.f};
+                        dp[h][t] = from_less<T> ? less_dp : f32x4{0.f, 0.f, 0.f, 0.f};
                     }
 #pragma unroll
                     for (int c = 0; c < KC; ++c) {
@@ -546,7 +548,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const float x = away() ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
-                            float power = s[h][t][r] * scale2 + x, d = dp[h][t][r];
+                            float power = s[h][t][r] * scale2 + (from_less<T> ? x : x + less_s[r]), d = from_less<T> ? dp[h][t][r] : dp[h][t][r] + less_dp[r];
                             if constexpr (mask()) {
                                 // a key that the row does not see, the keys behind the last, the rows behind the last
                                 const int key = wkey + 16 * t + j, row = r0 + 32 * c2 + 16 * h + 4 * g + r;
