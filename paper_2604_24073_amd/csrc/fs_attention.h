@@ -75,21 +75,18 @@ __device__ __forceinline__ void as_operand(piece<float> &p, const f32x4 &lo, con
     }
 }
 
-// The same with what the rounding left out as a second operand: the two together hold a value to 16 bits.
-__device__ __forceinline__ void as_operands(piece<bf16_t> &p, piece<bf16_t> &rest, const f32x4 &lo, const f32x4 &hi) {
+// The same, leaving in lo and hi what the rounding took off: of bf16 three such terms hold a value to its 24 bits.
+__device__ __forceinline__ void take_operand(piece<bf16_t> &p, f32x4 &lo, f32x4 &hi) {
     as_operand(p, lo, hi);
     const u32x4 w = __builtin_bit_cast(u32x4, p.v);
-    f32x4 a, b;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        a[2 * i] = lo[2 * i] - bf16_lo(w[i]);
-        a[2 * i + 1] = lo[2 * i + 1] - bf16_hi(w[i]);
-        b[2 * i] = hi[2 * i] - bf16_lo(w[2 + i]);
-        b[2 * i + 1] = hi[2 * i + 1] - bf16_hi(w[2 + i]);
+        lo[2 * i] -= bf16_lo(w[i]);
+        lo[2 * i + 1] -= bf16_hi(w[i]);
+        hi[2 * i] -= bf16_lo(w[2 + i]);
+        hi[2 * i + 1] -= bf16_hi(w[2 + i]);
     }
-    as_operand(rest, a, b);
 }
-__device__ __forceinline__ void as_operands(piece<float> &p, piece<float> &, const f32x4 &lo, const f32x4 &hi) { as_operand(p, lo, hi); }
 
 // ---- tiles in LDS -------------------------------------------------------------------------------------------------------------
 // kTile rows of DH columns (the head's width rounded up to 32, 64 or 128; zeros behind it), rows 16 bytes further apart than
