@@ -97,6 +97,7 @@ size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
 #define FS_MAX_BIAS_BUCKETS 1024
 #define FS_MAX_BIAS_DISTANCES 4096
 #define FS_MAX_ROW_STRIDE (1 << 22)       /* elements */
+#define FS_HIDDEN_BIAS (-40000.f)         /* a bias so low hides its pairs */
 
 /* Attention of each user's query rows over the user's keys and values, with a learned bias for the bucket that the distance
  * between the two lies in:
@@ -106,8 +107,9 @@ size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
  * of the history: with nk keys in use and nq query rows, row i stands at position nk - nq + i, key j at j.  For a batch
  * that attends to itself q_offsets and kv_offsets are the same.
  *   causal == 1: row i sees the keys up to its own position; == 0: all keys in use.  A row that sees no key (there are more
- *         query rows than keys, or every bias it meets is -infinity) gives zeros, and no gradient.  What a row does not see
- *         does not reach it, infinities and NaN included.
+ *         query rows than keys, or every bias it meets hides) gives zeros, and no gradient.  What a row does not see does not
+ *         reach it, infinities and NaN included.  A bias of FS_HIDDEN_BIAS or less, -infinity and every type's lowest value
+ *         among them, hides its pairs.
  *   q [n_q, heads, head_dim], k and v [n_kv, kv_heads, head_dim] of dt, heads of a row next to each other, rows q_stride,
  *         k_stride, v_stride elements apart; query heads h .. h + heads/kv_heads - 1 share a key head
  *   bias  [num_buckets, heads] fp32 (NULL: none), bucket_of int32: the bucket of each distance, tabulated by the caller -
@@ -125,9 +127,10 @@ size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
  *   work  fs_jagged_attention_work_bytes(args) bytes, 16-byte aligned, contents irrelevant (0 bytes and NULL but for the form
  *         above)
  * scale is positive.  Scores, softmax and sums are in fp32; P and dS are rounded to dt where they go into a product.  head_dim
- * a multiple of 4 (fp32) / 8 (bf16), at most FS_MAX_HEAD_DIM.  (rows / 64 + batch) * heads < 2^24, a user has fewer than 2^30 rows.  Boundaries that do not ascend
- * from 0 to n_q (n_kv) and lengths that do not fit their room are reported as FS_ERANGE by fs_check_async; out of the user
- * concerned is not written or is that of the keys there are. */
+ * a multiple of 4 (fp32) / 8 (bf16), at most FS_MAX_HEAD_DIM; strides of q, k and v at most FS_MAX_ROW_STRIDE.
+ * (rows / 64 + batch) * heads < 2^24, and a user has fewer than 2^30 rows.  Boundaries that do not ascend from 0 to n_q (n_kv)
+ * and lengths that do not fit their room are reported as FS_ERANGE by fs_check_async; out of the user concerned is not written
+ * or is that of the keys there are. */
 typedef struct fs_attention_args {
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;

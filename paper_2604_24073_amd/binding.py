@@ -908,6 +908,7 @@ def fs_block_norm_backward(ctx: Context, dy: Optional[torch.Tensor], dh: Optiona
 
 
 FS_MAX_HEAD_DIM, FS_MAX_BIAS_BUCKETS, FS_MAX_BIAS_DISTANCES, FS_MAX_ROW_STRIDE = 128, 1024, 4096, 1 << 22
+FS_HIDDEN_BIAS = -40000.0      # a bias so low hides its pairs
 
 
 def _attention_record(ctx, q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale):

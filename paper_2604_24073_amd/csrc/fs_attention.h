@@ -369,6 +369,11 @@ __device__ __forceinline__ void check_layout(const attn_params &p, int slot, int
 }
 
 // ---- the bias by distance -----------------------------------------------------------------------------------------------------
+// A bias as the kernels add it, times log2 e.  One so low that 24 bits have no room for a score beside it hides its pairs like
+// -inf: what a row that met nothing else would get of it is the roundings of sums of that size, not a softmax.
+constexpr float kHidden = FS_HIDDEN_BIAS;
+__device__ __forceinline__ float bias_power(float b) { return b <= kHidden ? neg_inf() : b * kLog2e; }
+
 // at[zero + d] is the bias of distance d (times log2 e) for the distances a workgroup meets, kPad further on either side: the
 // distances of a tile lie within kPad of one that counts, so that nobody has to bring a distance into range.
 template <int kPad>
@@ -382,7 +387,7 @@ struct strip {
     // what the table has for a distance, and the bucket that is: -1 where it is none
     __device__ __forceinline__ int entry(const attn_params &p, int d) const { return p.bucket_of[min(max(d, low), high) - low]; }
     static __device__ __forceinline__ int bucket(const attn_params &p, int k) { return k < p.buckets ? max(k, -1) : -1; }
-    // Distances from `from` to `to` (and kPad around) are met.  Returns whether any bias of them hides (is -inf); has a barrier.
+    // Distances from `from` to `to` (and kPad around) are met.  Returns whether any bias of them hides (is -inf then); has a barrier.
     __device__ __forceinline__ bool fill(const attn_params &p, int head, float *lds, int from, int to) {
         at = lds;
         high = p.distances - 1;
@@ -395,7 +400,7 @@ struct strip {
             if (p.bias) {
                 const int k = bucket(p, entry(p, d));
                 if (k < 0) atomicOr(p.flags, kFlagRowRange);
-                else x = p.bias[(int64_t)k * p.heads + head] * kLog2e;
+                else x = bias_power(p.bias[(int64_t)k * p.heads + head]);
             }
             at[zero + d] = x;
             hides |= x == neg_inf();

@@ -157,7 +157,8 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
                 top = column_max(top);
                 const bool behind = top > ahead[t];
                 if (__any(behind)) {
-                    const float step = behind ? top : 0.f, shrink = behind ? __builtin_amdgcn_exp2f(-step) : 1.f;
+                    // at first, where top may be anything, there is nothing to shrink yet
+                    const float step = behind ? top : 0.f, shrink = __builtin_amdgcn_exp2f(-fmaxf(step, 0.f));
                     m[t] += step;
                     less[t] = -m[t] * inv_scale2;
                     ahead[t] = behind ? 8.f : ahead[t];
@@ -346,7 +347,7 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
             const bool none = bucket < 0 || bucket >= p.buckets;
             if (p.bias && none) atomicOr(p.flags, kFlagRowRange);
             for (int h = 0; h < p.group; ++h) {
-                const float b = none ? 0.f : p.bias[(int64_t)bucket * p.heads + kvh * p.group + h] * kLog2e;
+                const float b = none ? 0.f : bias_power(p.bias[(int64_t)bucket * p.heads + kvh * p.group + h]);
                 bias_lds[threadIdx.x * p.group + h] = b;
                 hides |= b == neg_inf();
             }
@@ -688,8 +689,8 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
             constexpr int QT = qt();
             const size_t lds = 2 * tile_buffers<T, DH> * sizeof(tile<T, DH>) + 2 * kAttnWaves * sizeof(uint32_t) +
                                strip<fwd_rows(QT) + kTile>::entries(p.distances, a.causal != 0) * sizeof(float);
-            return launch_attention(ctx, attn_forward_kernel<T, DH, QT, exact()>, attn_slots(a.n_q, a.batch, QT == 1 ? 6 : 7) * a.heads, lds, s,
-                                    "attn_forward", p);
+            return launch_attention(ctx, attn_forward_kernel<T, DH, QT, exact()>,
+                                    attn_slots(a.n_q, a.batch, QT == 1 ? 6 : 7) * a.heads, lds, s, "attn_forward", p);
         };
         const auto rows = [&](auto exact) {
             return forward_qt(a) == 2 ? run(std::integral_constant<int, 2>(), exact) : run(std::integral_constant<int, 1>(), exact);

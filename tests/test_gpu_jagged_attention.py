@@ -233,9 +233,40 @@ def test_a_bias_that_hides(ctx, dtype, causal):
     c.check(ctx, grads=False, max_q=3)
 
 
-def finite_rows(c, rows):
-    """Case c without the users' rows in `rows` counted: what everything else has to come out as."""
-    return [r for r in range(c.q.shape[0]) if r not in rows]
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+def test_masks_of_a_types_lowest_value(ctx, dtype, causal):
+    lows = [-4e4, -65504.0, -1e9, torch.finfo(BF16).min, torch.finfo(F32).min]
+    for few in (0, 3):
+        lens = ([3, 2, 1], [300, 600, 70]) if few else ([100, 65, 1, 30], None)
+        c, d = (Case(*lens, dtype=dtype, causal=causal, buckets=8, distances=20) for _ in range(2))
+        for i, low in enumerate(lows):
+            c.bias[1 + i], d.bias[1 + i] = low, -np.inf
+        c.bias[0, 1], d.bias[0, 1] = lows[-1], -np.inf
+        got, want = c.forward(ctx, keep=True, max_q=few), d.forward(ctx, keep=True, max_q=few)
+        back, ref = c.backward(ctx, got), d.backward(ctx, want)
+        for x, y in ((got, want), (back, ref)):
+            assert all(torch.equal(x[n], y[n]) for n in y if y[n] is not None)
+        if not few:
+            d.check(ctx)
+    # low, but not that low: what a row meets nothing else of is what it sees
+    c = Case([100, 65, 1, 30], dtype=dtype, causal=causal, buckets=3, distances=20)
+    c.bias[:] = -1e4
+    c.check(ctx)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shift", [-3000.0, -200.0, 200.0, 3000.0])
+def test_scores_far_from_zero(ctx, dtype, shift):
+    """All scores of a row far below or above zero, in the first tile and in later ones."""
+    c = Case([100, 300], dtype=dtype, buckets=3, distances=200)
+    c.bias += shift
+    c.check(ctx)
+    c.bias += torch.tensor([0.0, shift, -shift])[:, None]
+    c.check(ctx)
+    c = Case([2, 1], [300, 700], dtype=dtype, buckets=3, distances=200)
+    c.bias += shift
+    c.check(ctx, grads=False, max_q=2)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
