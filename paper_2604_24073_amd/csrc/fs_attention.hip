@@ -646,8 +646,15 @@ int64_t split_rows(const fs_attention_args &a) {       // rows of partial result
     return attn_slots(a.n_kv, a.batch, split_shift(a)) * a.kv_heads * a.max_q * (a.heads / a.kv_heads);
 }
 
-// QT = 2 halves what a score reads from LDS; with short histories half of its rows would be none
-int forward_qt(const fs_attention_args &a) { return a.n_q >= 128 * a.batch ? 2 : 1; }
+// Query rows of a wavefront: 32 halve what a score reads from LDS, which counts the more the wider the rows; 16 leave registers
+// for five wavefronts a SIMD in place of three and fewer rows that are none.  In us, with 16 and with 32 rows:
+//   bf16, 64 columns: 280 / 305 (1000 histories of up to 400), 835 / 845 (1024 of 256 on average), 1787 / 1665 (64 of 4000 up)
+//   bf16, 128 columns: 342 / 321 (300 of 200 up), 1703 / 1443 (64 of 2000 up);  bf16, 32: 494 / 540 (1024 of 256 on average),
+//   1043 / 1053 (64 of 4000 up);  fp32, 64: 240 / 263 (300 of 200 up), 455 / 463 (64 of 1000 up);  fp32, 128: 1939 / 1729 (32
+//   of 2000 up)
+template <typename T, int DH>
+constexpr bool wide_enough = DH >= (sizeof(T) == 2 ? 64 : 128);
+bool long_enough(const fs_attention_args &a) { return a.n_q >= 256 * a.batch; }
 
 }  // namespace
 
@@ -693,7 +700,10 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
                                     attn_slots(a.n_q, a.batch, QT == 1 ? 6 : 7) * a.heads, lds, s, "attn_forward", p);
         };
         const auto rows = [&](auto exact) {
-            return forward_qt(a) == 2 ? run(std::integral_constant<int, 2>(), exact) : run(std::integral_constant<int, 1>(), exact);
+            if constexpr (wide_enough<T, DH>) {
+                if (long_enough(a)) return run(std::integral_constant<int, 2>(), exact);
+            }
+            return run(std::integral_constant<int, 1>(), exact);
         };
         if constexpr (sizeof(T) == 2) {
             if (p.out_f32) return rows(std::true_type());

@@ -669,16 +669,27 @@ __global__ __launch_bounds__(256) void attn_bias_sum_kernel(const double *__rest
     dbias[(k % buckets) * heads + k / buckets] = (float)s;
 }
 
-// keys of a wavefront: twice sixteen halve what a score reads from LDS; fp32 and the widest rows have no registers for them
+// Whether a wavefront may have 32 query rows, or 32 keys: they halve what a score reads from LDS, and there are registers for
+// them with bf16 rows of up to 64 columns.  Sixteen leave registers for more wavefronts, and fewer rows that are none.
 template <typename T, int DH>
-constexpr int key_sixteens = sizeof(T) == 2 && DH <= 64 ? 2 : 1;
+constexpr bool two_sixteens = sizeof(T) == 2 && DH <= 64;
 
 }  // namespace
 
 namespace fs {
 
-// query rows of a wavefront of attn_dq_kernel: as for the keys, where the users have rows for them on average
-static int dq_shift(const attn_params &p, int dt) { return dt == FS_BF16 && p.width <= 64 && p.n_q >= 128 * p.batch ? 7 : 6; }
+// Query rows of a workgroup of attn_dq_kernel, by the average of the histories.  In us, with 16 and with 32 rows a wavefront:
+//   32 columns: 800 / 871 (1024 histories of 256 on average), 251 / 258 (300 of 400 up), 1518 / 1449 (64 of 4000 up)
+//   64 columns: 475 / 407 (1000 of up to 400), 1274 / 1004 (1024 of 256 on average), 2391 / 1706 (64 of 4000 up)
+static int dq_shift(const attn_params &p, int dt) {
+    return dt == FS_BF16 && p.width <= 64 && p.n_q >= (p.width <= 32 ? 1024 : 128) * p.batch ? 7 : 6;
+}
+// Keys of a workgroup of attn_dkv_kernel.  In us, with 16 and with 32 keys a wavefront:
+//   32 columns: 598 / 683 (1024 histories of 256 on average), 172 / 187 (300 of 400 up), 1250 / 1259 (64 of 4000 up)
+//   64 columns: 344 / 390 (1000 of up to 400), 1010 / 996 (1024 of 256 on average), 2107 / 1845 (64 of 4000 up)
+static int dkv_shift(const attn_params &p, int dt) {
+    return dt == FS_BF16 && p.width > 32 && p.width <= 64 && p.n_kv >= 256 * p.batch ? 7 : 6;
+}
 
 // scratch: delta, then the bias's sums of every workgroup, then those of the cuts
 static size_t delta_bytes(const attn_params &p) { return ((size_t)p.heads * p.n_q * sizeof(float) + 255) / 256 * 256; }
@@ -702,7 +713,7 @@ int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void
     if (p.batch > 0) {
         const int rc = by_head(dt, p.width, [&](auto *t, auto dh) -> int {
             using T = std::remove_pointer_t<decltype(t)>;
-            constexpr int DH = dh(), KT = key_sixteens<T, DH>, B = tile_buffers<T, DH>;
+            constexpr int DH = dh(), B = tile_buffers<T, DH>;
             const auto query_rows = [&](auto qt) {
                 constexpr int QT = qt();
                 const size_t bias = strip<16 * kAttnWaves * QT + kTile>::entries(p.distances, causal);
@@ -710,15 +721,22 @@ int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void
                 return launch_attention(ctx, attn_dq_kernel<T, DH, QT>, slots * p.heads, lds, s, "attn_dq", p);
             };
             int done = FS_OK;
-            if constexpr (key_sixteens<T, DH> == 2)
+            if constexpr (two_sixteens<T, DH>)
                 done = shift == 7 ? query_rows(std::integral_constant<int, 2>()) : query_rows(std::integral_constant<int, 1>());
             else
                 done = query_rows(std::integral_constant<int, 1>());
             if (done != FS_OK) return done;
-            const size_t keys = 2 * B * sizeof(tile<T, DH>) + (8 * kTile + 2 * kAttnWaves) * sizeof(float) +
-                                strip<16 * kAttnWaves * KT + kTile>::entries(p.distances, causal) * sizeof(float);
-            return launch_attention(ctx, attn_dkv_kernel<T, DH, KT>, attn_slots(p.n_kv, p.batch, KT == 1 ? 6 : 7) * (p.heads / p.group), keys,
-                                    s, "attn_dkv", p);
+            const auto keys = [&](auto kt) {
+                constexpr int KT = kt();
+                const size_t lds = 2 * B * sizeof(tile<T, DH>) + (8 * kTile + 2 * kAttnWaves) * sizeof(float) +
+                                   strip<16 * kAttnWaves * KT + kTile>::entries(p.distances, causal) * sizeof(float);
+                return launch_attention(ctx, attn_dkv_kernel<T, DH, KT>,
+                                        attn_slots(p.n_kv, p.batch, KT == 1 ? 6 : 7) * (p.heads / p.group), lds, s, "attn_dkv", p);
+            };
+            if constexpr (two_sixteens<T, DH> && DH > 32) {
+                if (dkv_shift(p, dt) == 7) return keys(std::integral_constant<int, 2>());
+            }
+            return keys(std::integral_constant<int, 1>());
         });
         if (rc != FS_OK) return rc;
     }

@@ -113,10 +113,12 @@ def test_bias_tables(ctx, dtype, causal, buckets, distances):
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("run", [17, 50, 134])
-def test_buckets_that_begin_anywhere_in_a_tile(ctx, dtype, causal, run):
-    """Runs of distances that share a bucket: none, one or several begin in a tile, at every place in it."""
+@pytest.mark.parametrize("width", [32, 64])
+def test_buckets_that_begin_anywhere_in_a_tile(ctx, dtype, causal, run, width):
+    """Runs of distances that share a bucket: none, one or several begin in a tile, at every place in it.  Wavefronts of 16 and,
+    with bf16 rows of 64 columns, of 32 query rows."""
     for shift in range(0, run, run // 8):
-        c = Case([650, 130], heads=1, kv_heads=1, width=32, dtype=dtype, causal=causal, buckets=100, distances=600, seed=shift)
+        c = Case([650, 130], heads=1, kv_heads=1, width=width, dtype=dtype, causal=causal, buckets=100, distances=600, seed=shift)
         c.bucket_of = ((torch.arange(c.bucket_of.shape[0]) + shift) // run).to(torch.int32)
         c.check(ctx)
 
@@ -137,6 +139,17 @@ def test_long_histories(ctx, dtype):
     """Long enough for the form with 32 rows a wavefront, for tiles behind the last distance and for many turns."""
     Case([700, 1500, 3, 260], heads=2, kv_heads=1, width=64, dtype=dtype, buckets=20, distances=200).check(ctx)
     Case([900], heads=2, kv_heads=1, width=64, dtype=dtype, buckets=20, distances=100, causal=False, scale=0.3).check(ctx)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("width", [32, 48, 128])
+def test_the_longer_the_histories_the_more_rows_at_a_time(ctx, dtype, causal, width):
+    """Averages on either side of every rule's border: 128, 256 and 1024 rows a user."""
+    for lens in ([255, 256], [257, 256], [100, 157], [1000, 1047], [1100, 950]):
+        c = Case(lens, heads=1, kv_heads=1, width=width, dtype=dtype, causal=causal, buckets=16, distances=150, seed=width)
+        c.bucket_of = (torch.arange(c.bucket_of.shape[0]) // 19 % 16).to(torch.int32)
+        c.check(ctx)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
