@@ -6,6 +6,13 @@
 // user and head, a wavefront 16 or 32 of them, and the keys come by in tiles of 64 through LDS, the next tile on its way while
 // this one is worked on.  The products are turned over: S^T = K Q^T and O^T = V^T P^T, so that a lane has one query row (two
 // with 32 rows), its m and l are a register each, and the scores stay in registers from one product to the other.
+//
+// Bound by the vector units, which have some ten instructions for a score beside the power's four slots, and by how little of
+// that the matrix units' time hides under with two wavefronts a SIMD (64 % and 34 % of the time, histories of 16384 rows).  160
+// histories with 150 k rows, 8 of them of 16384, 4 heads of 64 columns over 2 key heads, out unrounded for the bias's gradient:
+// 2.7 to 2.9 ms, 400 TFLOP/s of the formula's products and 800 of those that are made.  1024 histories with 262 k rows, 4 heads
+// of 32: 0.51 ms.  Tried without gain: the next tile's scores made beside this tile's powers (registers: a wavefront a SIMD
+// less, 0.51 ms to 0.62), priorities for wavefronts in their products.
 #include "fs_attention.h"
 
 using namespace fs;
@@ -268,8 +275,9 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
 // ---- few query rows -----------------------------------------------------------------------------------------------------------
 // Serving: a few new rows of each user against a long history.  What there is to do is to read k and v once, so the keys are
 // cut up: a workgroup has a chunk of one user's keys for all query rows and heads that share a key head (at most sixteen
-// columns of a product), its wavefronts take 64 keys each in turn, and what they have of m, l and o is put together, in the
-// workgroup first, then, where a user has several chunks, by a second launch.
+// columns of a product), its wavefronts take kSplitKeys keys each in turn, and what they have of m, l and o is put together, in
+// the workgroup first, then, where a user has several chunks, by a second launch.  Bound by the waits of one chunk, one behind
+// the other, more than by memory: 256 users with 93 k keys, 8 heads of 64 columns over 2, 47 MB: 20 us (2.4 TB/s) and 7.
 constexpr int kSplitCols = 16;
 constexpr int kSplitKeys = 32;                        // keys of a wavefront at a time
 constexpr int kSplitStep = kAttnWaves * kSplitKeys;   // keys of a workgroup at a time
@@ -557,11 +565,13 @@ constexpr int64_t kMaxGroups = 1 << 24;       // a launch has fewer than 2^32 th
 // Whether the rows are few enough for the split form: max_q of them, times the heads that share a key head, fit the sixteen
 // columns of a product.
 bool splits(const fs_attention_args &a) { return a.max_q > 0 && a.max_q * (int64_t)(a.heads / a.kv_heads) <= kSplitCols; }
-// Keys of a workgroup of the split form, as a power of two: as few as a workgroup takes at a time while that makes up to
-// eight workgroups a CU, more in larger caches, where more would only mean more to put together.
+// Keys of a workgroup of the split form, as a power of two: two turns of it while that makes up to sixteen workgroups a CU, more
+// in larger caches.  us with both launches, for 128 / 256 keys at least: 28.8 / 27.1 (256 users with 93 k keys, 8 heads of 64
+// columns over 2), 41.9 / 34.4 (64 with 98 k, 128 columns), 15.2 / 15.8 (32 with up to 8192 keys, 64 columns).  For up to 8 / 16 /
+// 32 workgroups a CU: 201 / 184 / 186 (256 users with 1.6 M keys, 64 columns).
 int split_shift(const fs_attention_args &a) {
     int shift = 8;
-    while (shift < 16 && (a.n_kv >> shift) * a.kv_heads > 8 * 256) ++shift;
+    while (shift < 16 && (a.n_kv >> shift) * a.kv_heads > 16 * 256) ++shift;
     return shift;
 }
 int padded(int width) { return width <= 32 ? 32 : width <= 64 ? 64 : 128; }

@@ -5,6 +5,11 @@
 // Two launches recompute the scores, one that owns query rows (dq, D and the bias) and one that owns keys (dk, dv): seven
 // products instead of the five of a single launch, and in exchange no sum crosses a workgroup but the bias's, so that nothing
 // is added up in an order that changes.  Both keep the scores in registers from product to product, as the forward pass does.
+//
+// Bound as the forward pass is.  160 histories with 150 k rows, 8 of them of 16384, 4 heads of 64 columns over 2 key heads:
+// query rows 2.3 to 2.5 ms (690 TFLOP/s of their three products), keys 3.4 to 3.5 (640 of their four).  1024 histories with
+// 262 k rows, 4 heads of 32: 0.81 and 0.60 ms, a third of the former the bias's sums (0.53
+// without), which tell the buckets of a tile apart.
 #include "fs_attention.h"
 
 using namespace fs;
