@@ -8,7 +8,7 @@
 // with 32 rows), its m and l are a register each, and the scores stay in registers from one product to the other.
 //
 // Bound by the vector units, which have some ten instructions for a score beside the power's four slots, and by how little of
-// that the matrix units' time hides under with two wavefronts a SIMD (64 % and 34 % of the time, histories of 16384 rows).  160
+// that the matrix units' time hides under with two wavefronts a SIMD (67 % and 36 % of the time, histories of 16384 rows).  160
 // histories with 150 k rows, 8 of them of 16384, 4 heads of 64 columns over 2 key heads, out unrounded for the bias's gradient:
 // 2.7 to 2.9 ms, 400 TFLOP/s of the formula's products and 800 of those that are made.  1024 histories with 262 k rows, 4 heads
 // of 32: 0.51 ms.  Tried without gain: the next tile's scores made beside this tile's powers (registers: a wavefront a SIMD
