@@ -13,6 +13,7 @@
  *     be larger than the row: q, k, v (and dq, dk, dv) may be the parts of one tensor.
  *   - Results do not vary from run to run: every sum is taken in a fixed order.
  *   - Entries of the records that a call does not read may hold anything.
+ *   - What a call writes lies over nothing that it reads or writes besides, but where it says that it may.
  */
 #ifndef FREESCALE_ENCODER_H
 #define FREESCALE_ENCODER_H
@@ -120,7 +121,7 @@ size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
  *   lse   [heads, n_q] fp32 (OPTIONAL; the backward pass reads it): log of the sum of exp(s_i), -infinity for a row that sees
  *         nothing
  *   out_f32 [n_q, heads, head_dim] fp32 (OPTIONAL, bf16 only): out before its rounding.  The backward pass reads it where it
- *         is given: without it, dbias carries the roundings of out.
+ *         is given: without it, dbias carries the roundings of out (and of P, behind the form for single tokens).
  *   max_q no user has more query rows than this (0: unknown).  With max_q * heads / kv_heads <= 16 the keys are cut up over
  *         the chip, which is the form for single tokens; a user with more rows is then reported as FS_ERANGE and its rows of
  *         out are left as they were.

@@ -496,6 +496,29 @@ def test_captured_and_replayed(ctx):
                 assert torch.equal(res[name], want[name]), (turn, name)
 
 
+def test_captured_with_large_tables_before_any_other_call(ctx):
+    """Kernels that ask for more LDS than they have unasked, first of all in a capture; replayed on other inputs."""
+    c = Case([150, 65], width=128, heads=2, kv_heads=1, buckets=512, distances=4000, causal=False)
+    lay, opt = c.layout(), c.options()
+    q, k, v, dout = (t.cuda() for t in (c.q, c.k, c.v, c.dout))
+
+    def train():
+        kept = fs.fs_jagged_attention(ctx, q, k, v, **lay, **opt, keep=True)
+        return {"out": kept["out"], **fs.fs_jagged_attention_backward(ctx, dout, kept, q, k, v, **lay, **opt)}
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        res = train()
+    for turn in range(3):
+        for t in (q, k, v, dout):
+            t.copy_(torch.randn(t.shape, generator=torch.Generator().manual_seed(turn)).to(t.dtype))
+        graph.replay()
+        want = train()
+        for name in want:
+            assert torch.equal(res[name], want[name]), (turn, name)
+
+
 @pytest.mark.parametrize("users", [64, 65, 66, 129, 200, 256, 1000, 4097])
 def test_many_users(ctx, users):
     """Every user is found, the last ones among them, by tiles of rows, of keys and by row."""
