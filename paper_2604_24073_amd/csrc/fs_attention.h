@@ -147,10 +147,6 @@ __device__ __forceinline__ uint32_t clean_word(uint32_t w, bool &any) {
     }
 }
 
-// tiles of a kind in LDS: one to work on and one to fill, but for the widest rows, of which two pairs would not fit
-template <typename T, int DH>
-constexpr int tile_buffers = sizeof(T) * DH >= 512 ? 1 : 2;
-
 // Rows of a head as the memory unit sees them: what it reads behind the last byte is zeros, and nothing there is touched.
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 struct window {
@@ -374,6 +370,10 @@ __device__ __forceinline__ void check_layout(const attn_params &p, int slot, int
 constexpr float kHidden = FS_HIDDEN_BIAS;
 __device__ __forceinline__ float bias_power(float b) { return b <= kHidden ? neg_inf() : b * kLog2e; }
 
+// What a strip needs beside the distances that count, for workgroups of 64 QT query rows: a wavefront's tile reaches 62 + 16 QT
+// distances beyond one of them, and there may be up to 64 QT - 1 rows behind the last.
+constexpr int row_pad(int qt) { return 64 * qt > kTile + 16 * qt ? 64 * qt : kTile + 16 * qt; }
+
 // at[zero + d] is the bias of distance d (times log2 e) for the distances a workgroup meets, kPad further on either side: the
 // distances of a tile lie within kPad of one that counts, so that nobody has to bring a distance into range.
 template <int kPad>
@@ -418,7 +418,7 @@ constexpr bool from_less = sizeof(T) == 2;
 // Wavefronts of a SIMD that a kernel is compiled for.  With two or more of them asked for, all of a wavefront's registers can be
 // named by every instruction, and the accumulators stay where the vector units can read them.
 template <typename T, int DH>
-constexpr int attn_waves = sizeof(T) * DH <= 128 ? 2 : 1;
+constexpr int attn_waves = sizeof(T) * DH <= 256 ? 2 : 1;
 
 // ---- host side --------------------------------------------------------------------------------------------------------------
 constexpr int kMaxLds = 160 * 1024;

@@ -27,14 +27,13 @@ constexpr int fwd_rows(int qt) { return 16 * kAttnWaves * qt; }
 // errors in them.  dbias is off by 6e-4 of itself with one term, 1e-6 with two, 4e-7 with three (1024 histories with 262 k rows,
 // 64 buckets, and histories of 16384 rows alike); the pass over the former, 4 heads of 32 columns, takes 0.41, 0.47 and 0.54 ms.
 template <typename T, int DH, int QT, bool EXACT>
-__global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forward_kernel(attn_params p) {
-    constexpr int kRows = fwd_rows(QT), kShift = QT == 1 ? 6 : 7, kPad = kRows + kTile;
+__global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_params p) {
+    constexpr int kRows = fwd_rows(QT), kShift = QT == 1 ? 6 : 7, kPad = row_pad(QT);
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kBufs = tile_buffers<T, DH>;
-    tile<T, DH> *kt = reinterpret_cast<tile<T, DH> *>(lds), *vt = kt + kBufs;
-    uint32_t *odd = reinterpret_cast<uint32_t *>(vt + kBufs);        // [2][wavefronts]: the tile had values that are no numbers
-    float *bias_lds = reinterpret_cast<float *>(odd + 2 * kAttnWaves);
+    tile<T, DH> &K = *reinterpret_cast<tile<T, DH> *>(lds), &V = (&K)[1];
+    uint32_t *odd = reinterpret_cast<uint32_t *>(&V + 1);            // [wavefronts]: the tile had values that are no numbers
+    float *bias_lds = reinterpret_cast<float *>(odd + kAttnWaves);
 
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int head = blockIdx.x % p.heads;
@@ -86,13 +85,12 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
     // a tile in which some rows do not see all keys: what they do not see must not reach them, not even as 0 * NaN
     const auto edge = [&](int n) { return hides || (p.causal && (n + 1) * kTile - 1 > pos0); };
     const auto stage = [&](int n) {
-        if (kBufs == 1) __syncthreads();
-        kr.store(kt[n & (kBufs - 1)]);
+        kr.store(K);
         if (edge(n)) {
             const bool any = __any(vr.clean());
-            if (lane == 0) odd[(n & 1) * kAttnWaves + w] = any;
+            if (lane == 0) odd[w] = any;
         }
-        vr.store(vt[n & (kBufs - 1)]);
+        vr.store(V);
     };
     if (tiles) stage(0);
     for (int n = 0; n < tiles; ++n) {
@@ -102,7 +100,6 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
             kr.load(kbase + (int64_t)(key0 + kTile) * p.k_stride, p.k_stride, u.nk - key0 - kTile);
             vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile);
         }
-        const tile<T, DH> &K = kt[n & (kBufs - 1)], &V = vt[n & (kBufs - 1)];
         if (wrow < u.nq && !(p.causal && key0 > wpos + 16 * QT - 1)) {
             f32x4 s[QT][4];
 #pragma unroll
@@ -220,7 +217,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
             settle();
             if (edge(n)) {
                 uint32_t any = 0;
-                for (int x = 0; x < kAttnWaves; ++x) any |= odd[(n & 1) * kAttnWaves + x];
+                for (int x = 0; x < kAttnWaves; ++x) any |= odd[x];
                 if (any) {
                     // the values left out of the product, key by key, for the rows that see them
                     const int keys = u.nk - key0 < kTile ? u.nk - key0 : kTile;
@@ -244,7 +241,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_forwar
                 }
             }
         }
-        if (n + 1 < tiles) stage(n + 1);
+        if (n + 1 < tiles) {
+            __syncthreads();
+            stage(n + 1);
+        }
     }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -663,7 +663,7 @@ int64_t split_rows(const fs_attention_args &a) {       // rows of partial result
 //   1043 / 1053 (64 of 4000 up);  fp32, 64: 240 / 263 (300 of 200 up), 455 / 463 (64 of 1000 up);  fp32, 128: 1939 / 1729 (32
 //   of 2000 up)
 template <typename T, int DH>
-constexpr bool wide_enough = DH >= (sizeof(T) == 2 ? 64 : 128);
+constexpr bool wide_enough = sizeof(T) == 2 && DH == 64;
 bool long_enough(const fs_attention_args &a) { return a.n_q >= 256 * a.batch; }
 
 }  // namespace
@@ -704,8 +704,8 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
         }
         const auto run = [&](auto qt, auto exact) {
             constexpr int QT = qt();
-            const size_t lds = 2 * tile_buffers<T, DH> * sizeof(tile<T, DH>) + 2 * kAttnWaves * sizeof(uint32_t) +
-                               strip<fwd_rows(QT) + kTile>::entries(p.distances, a.causal != 0) * sizeof(float);
+            const size_t lds = 2 * sizeof(tile<T, DH>) + kAttnWaves * sizeof(uint32_t) +
+                               strip<row_pad(QT)>::entries(p.distances, a.causal != 0) * sizeof(float);
             return launch_attention(ctx, attn_forward_kernel<T, DH, QT, exact()>,
                                     attn_slots(a.n_q, a.batch, QT == 1 ? 6 : 7) * a.heads, lds, s, "attn_forward", p);
         };

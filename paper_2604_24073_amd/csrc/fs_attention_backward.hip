@@ -183,13 +183,12 @@ __device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, co
 // QT: sixteens of query rows of a wavefront
 template <typename T, int DH, int QT>
 __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_kernel(attn_params p) {
-    constexpr int kRows = 16 * kAttnWaves * QT, kShift = QT == 1 ? 6 : 7, kPad = kRows + kTile;
+    constexpr int kRows = 16 * kAttnWaves * QT, kShift = QT == 1 ? 6 : 7, kPad = row_pad(QT);
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kBufs = tile_buffers<T, DH>;
-    tile<T, DH> *kt = reinterpret_cast<tile<T, DH> *>(lds), *vt = kt + kBufs;
-    float *mark = reinterpret_cast<float *>(vt + kBufs);                          // [2][kTile]
-    float *skew = mark + 2 * kTile;                                               // [wavefronts][kSkew]
+    tile<T, DH> &K = *reinterpret_cast<tile<T, DH> *>(lds), &V = (&K)[1];
+    float *mark = reinterpret_cast<float *>(&V + 1);                              // [kTile]
+    float *skew = mark + kTile;                                                   // [wavefronts][kSkew]
     float *bias_lds = skew + kAttnWaves * kSkew;
     const int entries = strip<kPad>::entries(p.distances, p.causal != 0);
     float *bins = bias_lds + entries;                                             // [wavefronts][buckets]
@@ -274,10 +273,9 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
     const auto stage = [&](int n) {
         // what a row does not see must not reach it, not even as 0 * NaN: the keys' infinities and NaN are taken out of the
         // product and put into the scores, where they are masked like any other
-        if (kBufs == 1) __syncthreads();
-        if (edge(n)) kr.clean(mark + (n & 1) * kTile);
-        kr.store(kt[n & (kBufs - 1)]);
-        vr.store(vt[n & (kBufs - 1)]);
+        if (edge(n)) kr.clean(mark);
+        kr.store(K);
+        vr.store(V);
     };
     if (tiles) stage(0);
     for (int n = 0; n < tiles; ++n) {
@@ -287,7 +285,6 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             kr.load(kbase + (int64_t)(key0 + kTile) * p.k_stride, p.k_stride, u.nk - key0 - kTile);
             vr.load(vbase + (int64_t)(key0 + kTile) * p.v_stride, p.v_stride, u.nk - key0 - kTile);
         }
-        const tile<T, DH> &K = kt[n & (kBufs - 1)], &V = vt[n & (kBufs - 1)];
         if (wrow < u.nq && !(p.causal && key0 > wpos + 16 * QT - 1)) {
             const int nearest = wpos - (key0 + kTile - 1), furthest = wpos + 16 * QT - 1 - key0;
             const bool all_far = nearest >= bias.high || furthest <= bias.low;
@@ -325,7 +322,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                         for (int t = 0; t < QT; ++t) mma(dp[t], a, of[t][c]);
                     }
                     f32x4 x;
-                    if constexpr (mask()) x = *reinterpret_cast<const f32x4 *>(mark + (n & 1) * kTile + 16 * k + 4 * g);
+                    if constexpr (mask()) x = *reinterpret_cast<const f32x4 *>(mark + 16 * k + 4 * g);
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
                         const int seen = p.causal ? min(wpos + 16 * t + j + 1, u.nk) : u.nk;     // keys that the row sees
@@ -371,7 +368,10 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                 }
             }
         }
-        if (n + 1 < tiles) stage(n + 1);
+        if (n + 1 < tiles) {
+            __syncthreads();
+            stage(n + 1);
+        }
     }
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -405,12 +405,11 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
     constexpr int kKeys = 16 * kAttnWaves * KT, kShift = KT == 1 ? 6 : 7, kPad = kKeys + kTile;
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
-    constexpr int kBufs = tile_buffers<T, DH>;
-    tile<T, DH> *qt = reinterpret_cast<tile<T, DH> *>(lds), *ot = qt + kBufs;
-    float *stats = reinterpret_cast<float *>(ot + kBufs);                         // [2][what scores are less by, -D][kTile]
-    float *mark = stats + 4 * kTile;                                              // [2][q, dout][kTile]
-    uint32_t *odd = reinterpret_cast<uint32_t *>(mark + 4 * kTile);               // [2][wavefronts]
-    float *bias_lds = reinterpret_cast<float *>(odd + 2 * kAttnWaves);
+    tile<T, DH> &Q = *reinterpret_cast<tile<T, DH> *>(lds), &O = (&Q)[1];
+    float *stats = reinterpret_cast<float *>(&O + 1);                             // [what scores are less by, -D][kTile]
+    float *mark = stats + 2 * kTile;                                              // [q, dout][kTile]
+    uint32_t *odd = reinterpret_cast<uint32_t *>(mark + 2 * kTile);               // [wavefronts]
+    float *bias_lds = reinterpret_cast<float *>(odd + kAttnWaves);
 
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15, w = wave_id();
     const int kv_heads = p.heads / p.group, kvh = blockIdx.x % kv_heads;
@@ -476,21 +475,19 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
     const auto edge = [&](int r0) {
         return key_first + kKeys > u.nk || r0 + kTile > u.nq || (p.causal && u.first + r0 < key_first + kKeys - 1);
     };
-    const auto stage = [&](int n, int r0, bool clean) {
-        const int b = n & 1;
-        if (kBufs == 1) __syncthreads();
+    const auto stage = [&](int r0, bool clean) {
         if (clean) {
-            qr.clean(mark + (2 * b) * kTile);
-            const bool any = __any(dr.clean(mark + (2 * b + 1) * kTile));
-            if (lane == 0) odd[b * kAttnWaves + w] = any;
+            qr.clean(mark);
+            const bool any = __any(dr.clean(mark + kTile));
+            if (lane == 0) odd[w] = any;
         }
-        qr.store(qt[n & (kBufs - 1)]);
-        dr.store(ot[n & (kBufs - 1)]);
+        qr.store(Q);
+        dr.store(O);
         if (w < 2) {
             const bool lse = w == 0, row = r0 + lane < u.nq;
             const float less = lse ? (stat == neg_inf() ? neg_inf() : -stat * (from_less<T> ? inv_scale : kLog2e)) : -stat;
             // rows that see nothing and rows that are none
-            stats[2 * b * kTile + threadIdx.x] = row ? less : lse ? neg_inf() : 0.f;
+            stats[threadIdx.x] = row ? less : lse ? neg_inf() : 0.f;
         }
     };
     const auto fill = [&](int head) {
@@ -501,15 +498,14 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
         begin_head();
         fetch();
         hides = fill(next_head);
-        stage(0, from, masked = edge(from) || hides);
+        stage(from, masked = edge(from) || hides);
     }
     for (int n = 0; n < turns; ++n) {
         __syncthreads();
-        const int b = n & 1, r0 = next_row, pos0 = u.first + r0, head = next_head;
+        const int r0 = next_row, pos0 = u.first + r0, head = next_head;
         if (r0 == from && n > 0) hides = fill(head);
         advance();
         if (n + 1 < turns) fetch();
-        const tile<T, DH> &Q = qt[n & (kBufs - 1)], &O = ot[n & (kBufs - 1)];
         // A tile has one form from its first product to its last, so that the products of one half run beside the powers of the
         // other: mask - some pairs are not seen, or are none; away - all distances are beyond the table.
         const auto work = [&](auto mask, auto away) {
@@ -525,7 +521,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     // dO V^T less D goes only into a product of such factors: it begins where the scores do, at -D
-                    const int at = 2 * b * kTile + 32 * c2 + 16 * h + 4 * g;
+                    const int at = 32 * c2 + 16 * h + 4 * g;
                     const f32x4 less_s = *reinterpret_cast<const f32x4 *>(stats + at);
                     const f32x4 less_dp = *reinterpret_cast<const f32x4 *>(stats + kTile + at);
 #pragma unroll
@@ -594,7 +590,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
             else work(std::false_type(), std::false_type());
             if (masked) {
                 uint32_t any = 0;
-                for (int x = 0; x < kAttnWaves; ++x) any |= odd[b * kAttnWaves + x];
+                for (int x = 0; x < kAttnWaves; ++x) any |= odd[x];
                 if (any) {
                     // the elements of dout left out of the product, row by row, for the keys that are seen
                     const int count = u.nq - r0 < kTile ? u.nq - r0 : kTile;
@@ -621,7 +617,8 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_ke
         if (n + 1 < turns) {
             // a head's first tile is put down before its bias is known to hide nothing
             masked = edge(next_row) || hides || next_row == from;
-            stage(n + 1, next_row, masked);
+            __syncthreads();
+            stage(next_row, masked);
         }
     }
 #pragma unroll
@@ -718,11 +715,11 @@ int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void
     if (p.batch > 0) {
         const int rc = by_head(dt, p.width, [&](auto *t, auto dh) -> int {
             using T = std::remove_pointer_t<decltype(t)>;
-            constexpr int DH = dh(), B = tile_buffers<T, DH>;
+            constexpr int DH = dh();
             const auto query_rows = [&](auto qt) {
                 constexpr int QT = qt();
-                const size_t bias = strip<16 * kAttnWaves * QT + kTile>::entries(p.distances, causal);
-                const size_t lds = 2 * B * sizeof(tile<T, DH>) + (2 * kTile + kAttnWaves * kSkew + bias + kAttnWaves * p.buckets) * sizeof(float);
+                const size_t bias = strip<row_pad(QT)>::entries(p.distances, causal);
+                const size_t lds = 2 * sizeof(tile<T, DH>) + (kTile + kAttnWaves * kSkew + bias + kAttnWaves * p.buckets) * sizeof(float);
                 return launch_attention(ctx, attn_dq_kernel<T, DH, QT>, slots * p.heads, lds, s, "attn_dq", p);
             };
             int done = FS_OK;
@@ -733,7 +730,7 @@ int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void
             if (done != FS_OK) return done;
             const auto keys = [&](auto kt) {
                 constexpr int KT = kt();
-                const size_t lds = 2 * B * sizeof(tile<T, DH>) + (8 * kTile + 2 * kAttnWaves) * sizeof(float) +
+                const size_t lds = 2 * sizeof(tile<T, DH>) + (4 * kTile + kAttnWaves) * sizeof(float) +
                                    strip<16 * kAttnWaves * KT + kTile>::entries(p.distances, causal) * sizeof(float);
                 return launch_attention(ctx, attn_dkv_kernel<T, DH, KT>,
                                         attn_slots(p.n_kv, p.batch, KT == 1 ? 6 : 7) * (p.heads / p.group), lds, s, "attn_dkv", p);
