@@ -2,16 +2,16 @@
 //
 //   s_ij = scale q_i . k_j + bias[bucket(pos_i - pos_j), head],  o_i = sum_j softmax(s_i)_j v_j
 //
-// One pass over the keys with the running maximum m and sum l of a row's softmax: a workgroup has 64 or 128 query rows of one
-// user and head, a wavefront 16 or 32 of them, and the keys come by in tiles of 64 through LDS, the next tile on its way while
-// this one is worked on.  The products are turned over: S^T = K Q^T and O^T = V^T P^T, so that a lane has one query row (two
-// with 32 rows), its m and l are a register each, and the scores stay in registers from one product to the other.
+// One pass over the keys with the running maximum m and sum l of a row's softmax: a workgroup has 64 query rows of one user
+// and head, a wavefront 16 of them, and the keys come by in tiles of 64 through LDS, the next tile on its way while
+// this one is worked on.  The products are turned over: S^T = K Q^T and O^T = V^T P^T, so that a lane has one query
+// row, its m and l are a register each, and the scores stay in registers from one product to the other.
 //
 // Bound by the vector units, which have some ten instructions for a score beside the power's four slots, and by how little of
-// that the matrix units' time hides under with two wavefronts a SIMD (67 % and 36 % of the time, histories of 16384 rows).  160
+// that the matrix units' time hides under (67 % and 36 % of the time, histories of 16384 rows, two wavefronts a SIMD).  160
 // histories with 150 k rows, 8 of them of 16384, 4 heads of 64 columns over 2 key heads, out unrounded for the bias's gradient:
 // 2.7 to 2.9 ms, 400 TFLOP/s of the formula's products and 800 of those that are made.  1024 histories with 262 k rows, 4 heads
-// of 32: 0.51 ms.  Tried without gain: the next tile's scores made beside this tile's powers (registers: a wavefront a SIMD
+// of 32: 0.50 ms.  Tried without gain: the next tile's scores made beside this tile's powers (registers: a wavefront a SIMD
 // less, 0.51 ms to 0.62), priorities for wavefronts in their products.
 #include "fs_attention.h"
 
@@ -19,16 +19,18 @@ using namespace fs;
 
 namespace {
 
-// query rows of a workgroup whose wavefronts have QT times sixteen
-constexpr int fwd_rows(int qt) { return 16 * kAttnWaves * qt; }
+// Sixteens of query rows of a wavefront.  Two halve what a score reads from LDS, but leave registers for fewer wavefronts and more
+// rows that are none.  us with one / two, bf16: 506 / 545 (1024 histories of 256 on average, 32 columns), 718 / 838 (64 columns),
+// 209 / 232 (300 of 400 up, 64), 1562 / 1600 (64 of 4000 up, 64), 2877 / 2809 (8 of 16384, 64), 1040 / 1750 (64 of 2000 up, 128).
+constexpr int QT = 1;
 
 // EXACT, of bf16 rows whose unrounded out is wanted: P goes into its product as three terms of bf16, which hold its 24 bits.  The
 // bias's gradient adds up differences of dO V^T and D = dO . out that cancel over a row, and an out made of rounded P leaves its
 // errors in them.  dbias is off by 6e-4 of itself with one term, 1e-6 with two, 4e-7 with three (1024 histories with 262 k rows,
-// 64 buckets, and histories of 16384 rows alike); the pass over the former, 4 heads of 32 columns, takes 0.41, 0.47 and 0.54 ms.
-template <typename T, int DH, int QT, bool EXACT>
+// 64 buckets, and histories of 16384 rows alike); the pass over the former, 4 heads of 32 columns, took 0.41, 0.47 and 0.54 ms.
+template <typename T, int DH, bool EXACT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_params p) {
-    constexpr int kRows = fwd_rows(QT), kShift = QT == 1 ? 6 : 7, kPad = row_pad(QT);
+    constexpr int kRows = 16 * kAttnWaves * QT, kShift = 6, kPad = row_pad(QT);
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
     tile<T, DH> &K = *reinterpret_cast<tile<T, DH> *>(lds), &V = (&K)[1];
@@ -656,16 +658,6 @@ int64_t split_rows(const fs_attention_args &a) {       // rows of partial result
     return attn_slots(a.n_kv, a.batch, split_shift(a)) * a.kv_heads * a.max_q * (a.heads / a.kv_heads);
 }
 
-// Query rows of a wavefront: 32 halve what a score reads from LDS, which counts the more the wider the rows; 16 leave registers
-// for five wavefronts a SIMD in place of three and fewer rows that are none.  In us, with 16 and with 32 rows:
-//   bf16, 64 columns: 280 / 305 (1000 histories of up to 400), 835 / 845 (1024 of 256 on average), 1787 / 1665 (64 of 4000 up)
-//   bf16, 128 columns: 342 / 321 (300 of 200 up), 1703 / 1443 (64 of 2000 up);  bf16, 32: 494 / 540 (1024 of 256 on average),
-//   1043 / 1053 (64 of 4000 up);  fp32, 64: 240 / 263 (300 of 200 up), 455 / 463 (64 of 1000 up);  fp32, 128: 1939 / 1729 (32
-//   of 2000 up)
-template <typename T, int DH>
-constexpr bool wide_enough = sizeof(T) == 2 && DH == 64;
-bool long_enough(const fs_attention_args &a) { return a.n_q >= 256 * a.batch; }
-
 }  // namespace
 
 extern "C" {
@@ -702,23 +694,16 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
             if (done != FS_OK || a.n_kv <= 1ll << p.split_shift) return done;     // nobody has several chunks
             return launch_attention(ctx, attn_join_kernel<T, DH>, ceil_div(a.n_q * a.heads, kAttnWaves), 0, s, "attn_join", p);
         }
-        const auto run = [&](auto qt, auto exact) {
-            constexpr int QT = qt();
+        const auto run = [&](auto exact) {
             const size_t lds = 2 * sizeof(tile<T, DH>) + kAttnWaves * sizeof(uint32_t) +
                                strip<row_pad(QT)>::entries(p.distances, a.causal != 0) * sizeof(float);
-            return launch_attention(ctx, attn_forward_kernel<T, DH, QT, exact()>,
-                                    attn_slots(a.n_q, a.batch, QT == 1 ? 6 : 7) * a.heads, lds, s, "attn_forward", p);
-        };
-        const auto rows = [&](auto exact) {
-            if constexpr (wide_enough<T, DH>) {
-                if (long_enough(a)) return run(std::integral_constant<int, 2>(), exact);
-            }
-            return run(std::integral_constant<int, 1>(), exact);
+            return launch_attention(ctx, attn_forward_kernel<T, DH, exact()>,
+                                    attn_slots(a.n_q, a.batch, 6) * a.heads, lds, s, "attn_forward", p);
         };
         if constexpr (sizeof(T) == 2) {
-            if (p.out_f32) return rows(std::true_type());
+            if (p.out_f32) return run(std::true_type());
         }
-        return rows(std::false_type());
+        return run(std::false_type());
     });
 }
 

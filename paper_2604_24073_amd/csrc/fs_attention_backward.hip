@@ -8,8 +8,8 @@
 //
 // Bound as the forward pass is.  160 histories with 150 k rows, 8 of them of 16384, 4 heads of 64 columns over 2 key heads:
 // query rows 2.3 to 2.5 ms (690 TFLOP/s of their three products), keys 3.4 to 3.5 (640 of their four).  1024 histories with
-// 262 k rows, 4 heads of 32: 0.81 and 0.60 ms, a third of the former the bias's sums (0.53
-// without), which tell the buckets of a tile apart.
+// 262 k rows, 4 heads of 32: 0.71 and 0.60 ms, a third of the former the bias's sums, which tell the buckets of a tile apart.
+// A second pair of tiles in LDS, to save a barrier a tile, was slower: fewer workgroups fit (0.81 and 0.60).
 #include "fs_attention.h"
 
 using namespace fs;
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
 // ---- keys ------------------------------------------------------------------------------------------------------------------------
 // KT: sixteens of keys of a wavefront
 template <typename T, int DH, int KT>
-__global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dkv_kernel(attn_params p) {
+__global__ __launch_bounds__(kAttnThreads, (KT == 1 && sizeof(T) * DH <= 128 ? 3 : attn_waves<T, DH>)) void attn_dkv_kernel(attn_params p) {
     constexpr int kKeys = 16 * kAttnWaves * KT, kShift = KT == 1 ? 6 : 7, kPad = kKeys + kTile;
     constexpr int KC = DH / 32, MT = DH / 16;
     extern __shared__ __align__(16) char lds[];
@@ -671,27 +671,23 @@ __global__ __launch_bounds__(256) void attn_bias_sum_kernel(const double *__rest
     dbias[(k % buckets) * heads + k / buckets] = (float)s;
 }
 
-// Whether a wavefront may have 32 query rows, or 32 keys: they halve what a score reads from LDS, and there are registers for
-// them with bf16 rows of up to 64 columns.  Sixteen leave registers for more wavefronts, and fewer rows that are none.
+// Whether a wavefront may have 32 query rows, or 32 keys: they halve what a score reads from LDS.  Narrower rows read less of it,
+// fp32 and wider rows have no registers for twice as many.
 template <typename T, int DH>
-constexpr bool two_sixteens = sizeof(T) == 2 && DH <= 64;
+constexpr bool two_sixteens = sizeof(T) == 2 && DH == 64;
 
 }  // namespace
 
 namespace fs {
 
-// Query rows of a workgroup of attn_dq_kernel, by the average of the histories.  In us, with 16 and with 32 rows a wavefront:
-//   32 columns: 800 / 871 (1024 histories of 256 on average), 251 / 258 (300 of 400 up), 1518 / 1449 (64 of 4000 up)
-//   64 columns: 475 / 407 (1000 of up to 400), 1274 / 1004 (1024 of 256 on average), 2391 / 1706 (64 of 4000 up)
-static int dq_shift(const attn_params &p, int dt) {
-    return dt == FS_BF16 && p.width <= 64 && p.n_q >= (p.width <= 32 ? 1024 : 128) * p.batch ? 7 : 6;
-}
-// Keys of a workgroup of attn_dkv_kernel.  In us, with 16 and with 32 keys a wavefront:
-//   32 columns: 598 / 683 (1024 histories of 256 on average), 172 / 187 (300 of 400 up), 1250 / 1259 (64 of 4000 up)
-//   64 columns: 344 / 390 (1000 of up to 400), 1010 / 996 (1024 of 256 on average), 2107 / 1845 (64 of 4000 up)
-static int dkv_shift(const attn_params &p, int dt) {
-    return dt == FS_BF16 && p.width > 32 && p.width <= 64 && p.n_kv >= 256 * p.batch ? 7 : 6;
-}
+// Query rows of a workgroup of attn_dq_kernel and keys of one of attn_dkv_kernel, as powers of two: with 32 a wavefront there are
+// fewer wavefronts, and more rows that are none in short histories.  us with 16 / 32, bf16 rows of 64 columns:
+//   query rows: 334 / 410 (2000 histories of up to 200), 361 / 413 (1000 of up to 400), 1006 / 1008 (1024 of 256 on average),
+//   316 / 311 (300 of 400 up), 1883 / 1724 (64 of 4000 up), 3422 / 2460 (8 of 16384);  keys, the same: 332 / 381, 357 / 385,
+//   1019 / 981, -, -, 4002 / 3524.  Query rows of 32 columns: 718 / 882 (1024 of 256 on average), 1342 / 1488 (64 of 4000 up).
+static bool may_have_two(const attn_params &p, int dt) { return dt == FS_BF16 && p.width > 32 && p.width <= 64; }
+static int dq_shift(const attn_params &p, int dt) { return may_have_two(p, dt) && p.n_q >= 512 * p.batch ? 7 : 6; }
+static int dkv_shift(const attn_params &p, int dt) { return may_have_two(p, dt) && p.n_kv >= 256 * p.batch ? 7 : 6; }
 
 // scratch: delta, then the bias's sums of every workgroup, then those of the cuts
 static size_t delta_bytes(const attn_params &p) { return ((size_t)p.heads * p.n_q * sizeof(float) + 255) / 256 * 256; }
@@ -735,7 +731,7 @@ int launch_attention_backward(fs_ctx *ctx, const attn_params &args, int dt, void
                 return launch_attention(ctx, attn_dkv_kernel<T, DH, KT>,
                                         attn_slots(p.n_kv, p.batch, KT == 1 ? 6 : 7) * (p.heads / p.group), lds, s, "attn_dkv", p);
             };
-            if constexpr (two_sixteens<T, DH> && DH > 32) {
+            if constexpr (two_sixteens<T, DH>) {
                 if (dkv_shift(p, dt) == 7) return keys(std::integral_constant<int, 2>());
             }
             return keys(std::integral_constant<int, 1>());
