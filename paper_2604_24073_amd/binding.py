@@ -8,6 +8,8 @@ the HIP library is missing, importing succeeds but the first call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
+import inspect
 import os
 import re
 from typing import Dict, NamedTuple, Optional, Sequence, Union
@@ -711,13 +713,32 @@ def _ctx_stream(ctx: Context, stream):
     return _stream(torch.cuda.current_stream(ctx.device) if stream is None else stream)
 
 
-def _scratch(ctx: Context, like: torch.Tensor, nbytes: int, handle) -> torch.Tensor:
-    """Scratch memory that is given back when the call has been enqueued: on the stream of the call, so that what torch makes
-    of it next waits for the call."""
-    work = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
-    if handle != _ctx_stream(ctx, None):
-        work.record_stream(torch.cuda.ExternalStream(handle or 0, device=ctx.device))
-    return work
+def _on_its_stream(call):
+    """A stream that a call names is the current one for as long as the call takes, so that torch takes scratch memory and
+    results from that stream's pool: memory of the current stream's pool may still be in use by what that stream has ahead,
+    which the named stream does not wait for.  Results belong to that stream as those of torch's own operators would: another
+    stream that reads them waits for it, and is named to record_stream before they are dropped."""
+    place = list(inspect.signature(call).parameters).index("stream") - 1          # behind ctx
+
+    @functools.wraps(call)
+    def run(ctx, *args, stream=None, **named):
+        if len(args) > place:
+            (stream,), args = args[place:], args[:place]
+        handle = None if stream is None else _ctx_stream(ctx, stream)
+        if stream is None or handle == _ctx_stream(ctx, None):
+            return call(ctx, *args, **named)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(handle or 0, device=ctx.device)
+        elif stream.device_index != ctx.device:
+            raise ValueError(f"stream: of cuda:{stream.device_index}, the context is on cuda:{ctx.device}")
+        with torch.cuda.stream(stream):
+            return call(ctx, *args, **named)
+    return run
+
+
+def _scratch(like: torch.Tensor, nbytes: int) -> torch.Tensor:
+    """Scratch memory that is given back when the call has been enqueued on the current stream, whose pool it is from."""
+    return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
 
 
 _DTYPE_CODES = {torch.float32: FS_F32, torch.bfloat16: FS_BF16}
@@ -781,6 +802,7 @@ def _matrix(what: str, t: torch.Tensor):
     return tuple(t.shape)
 
 
+@_on_its_stream
 def fs_rows_pack8(ctx: Context, rows: torch.Tensor, out: Optional[Rows8] = None, stream=None) -> Rows8:
     n, dim = _matrix("rows", rows)
     address, stride = _row_addr("rows", rows, (n, dim), rows.dtype, ctx.device)
@@ -793,6 +815,7 @@ def fs_rows_pack8(ctx: Context, rows: torch.Tensor, out: Optional[Rows8] = None,
     return out
 
 
+@_on_its_stream
 def fs_rows_unpack8(ctx: Context, packed: Rows8, dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None,
                     stream=None) -> torch.Tensor:
     n, dim = _matrix("packed.codes", packed.codes)
@@ -806,6 +829,7 @@ def fs_rows_unpack8(ctx: Context, packed: Rows8, dtype: torch.dtype = torch.floa
     return out
 
 
+@_on_its_stream
 def fs_block_norm(ctx: Context, x: torch.Tensor, a: Optional[torch.Tensor] = None, g: Optional[torch.Tensor] = None,
                   w_post: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
                   w_pre: Optional[torch.Tensor] = None, eps: float = 1e-6, pack: Sequence[str] = (),
@@ -845,6 +869,7 @@ def fs_block_norm(ctx: Context, x: torch.Tensor, a: Optional[torch.Tensor] = Non
     return res
 
 
+@_on_its_stream
 def fs_block_norm_backward(ctx: Context, dy: Optional[torch.Tensor], dh: Optional[torch.Tensor],
                            a: Union[torch.Tensor, Rows8, None] = None, g: Union[torch.Tensor, Rows8, None] = None,
                            y: Union[torch.Tensor, Rows8, None] = None, w_post: Optional[torch.Tensor] = None,
@@ -898,10 +923,9 @@ def fs_block_norm_backward(ctx: Context, dy: Optional[torch.Tensor], dh: Optiona
         rec.dw_post = _addr("dw_post", t, (dim,), f32, dev)
         res["dscale"] = t = given["dscale"] if "dscale" in given else torch.empty_like(scale)
         rec.dscale = _addr("dscale", t, (dim,), f32, dev)
-    handle = _ctx_stream(ctx, stream)
-    work = _scratch(ctx, some, ctx.lib.fs_block_norm_work_bytes(n, dim), handle)
+    work = _scratch(some, ctx.lib.fs_block_norm_work_bytes(n, dim))
     rec.work, rec.work_bytes = work.data_ptr(), work.numel()
-    rc = ctx.lib.fs_block_norm_backward(ctx.handle, rec, handle)
+    rc = ctx.lib.fs_block_norm_backward(ctx.handle, rec, _ctx_stream(ctx, stream))
     if rc:
         ctx.check(rc, "fs_block_norm_backward")
     return res
@@ -940,6 +964,7 @@ def _attention_record(ctx, q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_l
     return rec, shape, keys
 
 
+@_on_its_stream
 def fs_jagged_attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_offsets: torch.Tensor,
                         kv_offsets: torch.Tensor, bias: Optional[torch.Tensor] = None, bucket_of: Optional[torch.Tensor] = None,
                         kv_lengths: Optional[torch.Tensor] = None, causal: bool = True, scale: Optional[float] = None,
@@ -958,18 +983,18 @@ def fs_jagged_attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch
     if keep or "lse" in given:
         res["lse"] = t = given["lse"] if "lse" in given else torch.empty((shape[1], shape[0]), dtype=f32, device=q.device)
         rec.lse = _addr("lse", t, (shape[1], shape[0]), f32, dev)
-    handle = _ctx_stream(ctx, stream)
     if max_q:
         nbytes = ctx.lib.fs_jagged_attention_work_bytes(rec)
         if nbytes:
-            work = _scratch(ctx, q, nbytes, handle)
+            work = _scratch(q, nbytes)
             rec.work, rec.work_bytes = work.data_ptr(), work.numel()
-    rc = ctx.lib.fs_jagged_attention(ctx.handle, rec, handle)
+    rc = ctx.lib.fs_jagged_attention(ctx.handle, rec, _ctx_stream(ctx, stream))
     if rc:
         ctx.check(rc, "fs_jagged_attention")
     return res
 
 
+@_on_its_stream
 def fs_jagged_attention_backward(ctx: Context, dout: torch.Tensor, kept: Dict[str, torch.Tensor], q: torch.Tensor, k: torch.Tensor,
                                  v: torch.Tensor, q_offsets: torch.Tensor, kv_offsets: torch.Tensor,
                                  bias: Optional[torch.Tensor] = None, bucket_of: Optional[torch.Tensor] = None,
@@ -994,10 +1019,9 @@ def fs_jagged_attention_backward(ctx: Context, dout: torch.Tensor, kept: Dict[st
     if bias is not None:
         res["dbias"] = t = given["dbias"] if "dbias" in given else torch.empty_like(bias)
         rec.dbias = _addr("dbias", t, bias.shape, f32, dev)
-    handle = _ctx_stream(ctx, stream)
-    work = _scratch(ctx, q, ctx.lib.fs_jagged_attention_backward_work_bytes(rec), handle)
+    work = _scratch(q, ctx.lib.fs_jagged_attention_backward_work_bytes(rec))
     rec.work, rec.work_bytes = work.data_ptr(), work.numel()
-    rc = ctx.lib.fs_jagged_attention_backward(ctx.handle, rec, handle)
+    rc = ctx.lib.fs_jagged_attention_backward(ctx.handle, rec, _ctx_stream(ctx, stream))
     if rc:
         ctx.check(rc, "fs_jagged_attention_backward")
     return res
