@@ -78,14 +78,15 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_para
     // m: what the row's scores are less by (less: the same in the product's own terms); it follows the row's
     // maximum once that is 2^8 ahead, which is enough to keep the powers in range, and at once from the first key seen on
     float m[QT], l[QT], less[QT], ahead[QT];
-    const float inv_scale2 = 1.f / scale2;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         m[t] = l[t] = less[t] = 0.f;
         ahead[t] = neg_inf();
     }
-    // a tile in which some rows do not see all keys: what they do not see must not reach them, not even as 0 * NaN
-    const auto edge = [&](int n) { return hides || (p.causal && (n + 1) * kTile - 1 > pos0); };
+    // From this tile on some rows do not see all keys: what they do not see must not reach them, not even as 0 * NaN.  Below zero
+    // where the bias hides: one register tells both.
+    const int first_edge = hides ? -1 : p.causal ? max((pos0 + 1) >> 6, 0) : 0x7fffffff;
+    const auto edge = [&](int n) { return n >= first_edge; };
     const auto stage = [&](int n) {
         kr.store(K);
         if (edge(n)) {
@@ -141,6 +142,20 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_para
                             s[t][k][r] = s[t][k][r] * scale2 + (from_less<T> ? x : x - m[t]);
                         }
             }
+            if (first_edge < 0) {
+                // a hidden pair's product may be no number, and -inf added to that is none: its score is -inf all the same
+                const int near = min(max(nearest, bias.low - (62 + 16 * QT)), bias.high);
+                const float *b = bias.at + bias.zero + near + (j - 4 * g) + 12;
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        __builtin_amdgcn_sched_barrier(0);           // registers for four biases at a time
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (b[51 + 16 * t - 16 * k - r] == neg_inf()) s[t][k][r] = neg_inf();
+                    }
+            }
             if ((p.causal && key0 + kTile - 1 > wpos) || key0 + kTile > u.nk) {
 #pragma unroll
                 for (int t = 0; t < QT; ++t) {
@@ -166,7 +181,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_para
                     // at first, where top may be anything, there is nothing to shrink yet
                     const float step = behind ? top : 0.f, shrink = __builtin_amdgcn_exp2f(-fmaxf(step, 0.f));
                     m[t] += step;
-                    less[t] = -m[t] * inv_scale2;
+                    less[t] = -m[t] / scale2;
                     ahead[t] = behind ? 8.f : ahead[t];
                     l[t] *= shrink;
 #pragma unroll
@@ -393,8 +408,9 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const int key = 16 * k + 4 * g + r;
-                    const float x = s[k][r] * scale2 + b[-key * p.group];      // in the strip for every key of the step
-                    s[k][r] = key0 + key < seen ? x : neg_inf();
+                    const float x = b[-key * p.group];                         // in the strip for every key of the step
+                    // a hidden pair's product may be no number: -inf is not added to it but put in its place
+                    s[k][r] = key0 + key < seen && x != neg_inf() ? s[k][r] * scale2 + x : neg_inf();
                     top = fmaxf(top, s[k][r]);
                 }
             }

@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             // element r of s[t][k]: query row wrow + 16 t + j, key key0 + 16 k + 4 g + r
             f32x4 s[QT][4];
             // A tile has one form from its first product to its last, so that products run beside powers: mask - some pairs are
-            // not seen, or are none; away - all distances are beyond the table.
+            // not seen (whatever their product is, their score is -inf), or are none; away - all distances are beyond the table.
             const auto work = [&](auto mask, auto away) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                         for (int r = 0; r < 4; ++r) {
                             const float b = away() ? far : bb[51 + 16 * t - 16 * k - r];
                             float power = s[t][k][r] * scale2 + (from_less<T> ? b : b + less_s[t]), d = dp[t][r] - delta[t];
-                            if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen ? power + x[r] : neg_inf();
+                            if constexpr (mask()) power = key0 + 16 * k + 4 * g + r < seen && b != neg_inf() ? power + x[r] : neg_inf();
                             const float e = __builtin_amdgcn_exp2f(power);
                             if constexpr (mask()) d = e == 0.f ? 0.f : d;
                             s[t][k][r] = e * d;
@@ -553,11 +553,12 @@ void attn_dkv_kernel(attn_params p) {
                             const float x = away() ? far : bb[16 * (KT - 1) + 16 * h + r - 16 * t];
                             float power = s[h][t][r] * scale2 + (from_less<T> ? x : x + less_s[r]), d = from_less<T> ? dp[h][t][r] : dp[h][t][r] + less_dp[r];
                             if constexpr (mask()) {
-                                // a key that the row does not see, the keys behind the last, the rows behind the last
+                                // a key that the row does not see, a hidden pair (whatever its product is), the keys behind
+                                // the last, the rows behind the last
                                 const int key = wkey + 16 * t + j, row = r0 + 32 * c2 + 16 * h + 4 * g + r;
                                 int seen = p.causal ? min(u.first + row + 1, u.nk) : u.nk;
                                 seen = row < u.nq ? seen : 0;
-                                power = key < seen ? power + mq[r] : neg_inf();
+                                power = key < seen && x != neg_inf() ? power + mq[r] : neg_inf();
                                 d += mo[r];
                             }
                             const float e = __builtin_amdgcn_exp2f(power);
