@@ -508,67 +508,67 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
     }
 }
 
-// The chunks of a user put together: a wavefront has one query row of one head.
+// The chunks of a user put together: a wavefront has one query row of one head at a time.
 template <typename T, int DH>
 __global__ __launch_bounds__(kAttnThreads) void attn_join_kernel(attn_params p) {
     const int shift = p.split_shift, max_q = p.max_q;
     const int lane = threadIdx.x & 63;
-    const int64_t item = (int64_t)blockIdx.x * kAttnWaves + wave_id();
-    const int head = (int)(item % p.heads);
-    const int64_t at_row = item / p.heads;
-    if (at_row >= p.n_q) return;
-    // users without query rows begin where their successor does; the last one at or before a row is the row's
-    const int b = last_user(p.q_offsets, (int)p.batch, 0, 0, at_row);
-    const int64_t qa = p.q_offsets[b], qb = p.q_offsets[b + 1], ka = p.kv_offsets[b], kb = p.kv_offsets[b + 1];
-    if (qa < 0 || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv || at_row < qa || at_row >= qb || qb - qa > max_q ||
-        kb - ka > 0x3fffffff)
-        return;
-    const int nk = rows_in_use(p.kv_lengths ? p.kv_lengths[b] : kb - ka, (int)(kb - ka));
-    const int chunk = 1 << shift;
-    if (nk <= chunk) return;                            // written by the workgroup that had them all
-    const int row = (int)(at_row - qa);
-    const int kv_heads = p.heads / p.group, kvh = head / p.group, chunks = (nk + chunk - 1) >> shift;
-    const int64_t slot0 = (ka >> shift) + b;
-    const int64_t first = (slot0 * kv_heads + kvh) * (max_q * p.group) + row * p.group + head % p.group;
-    const int64_t apart = (int64_t)kv_heads * max_q * p.group;
-    float top = neg_inf();
-    for (int c = lane; c < chunks; c += 64) top = fmaxf(top, p.split_ml[2 * (first + c * apart)]);
+    for (int64_t item = (int64_t)blockIdx.x * kAttnWaves + wave_id(); item < p.n_q * p.heads; item += (int64_t)gridDim.x * kAttnWaves) {
+        const int head = (int)(item % p.heads);
+        const int64_t at_row = item / p.heads;
+        // users without query rows begin where their successor does; the last one at or before a row is the row's
+        const int b = last_user(p.q_offsets, (int)p.batch, 0, 0, at_row);
+        const int64_t qa = p.q_offsets[b], qb = p.q_offsets[b + 1], ka = p.kv_offsets[b], kb = p.kv_offsets[b + 1];
+        if (qa < 0 || qb > p.n_q || ka < 0 || kb < ka || kb > p.n_kv || at_row < qa || at_row >= qb || qb - qa > max_q ||
+            kb - ka > 0x3fffffff)
+            continue;
+        const int nk = rows_in_use(p.kv_lengths ? p.kv_lengths[b] : kb - ka, (int)(kb - ka));
+        const int chunk = 1 << shift;
+        if (nk <= chunk) continue;                           // written by the workgroup that had them all
+        const int row = (int)(at_row - qa);
+        const int kv_heads = p.heads / p.group, kvh = head / p.group, chunks = (nk + chunk - 1) >> shift;
+        const int64_t slot0 = (ka >> shift) + b;
+        const int64_t first = (slot0 * kv_heads + kvh) * (max_q * p.group) + row * p.group + head % p.group;
+        const int64_t apart = (int64_t)kv_heads * max_q * p.group;
+        float top = neg_inf();
+        for (int c = lane; c < chunks; c += 64) top = fmaxf(top, p.split_ml[2 * (first + c * apart)]);
 #pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
-    const float base = top == neg_inf() ? 0.f : top;
-    constexpr int kMine = DH < kWave ? 1 : DH / kWave, kAtOnce = 8;
-    float o[kMine] = {}, sum = 0.f;
-    for (int c0 = 0; c0 < chunks; c0 += kAtOnce) {          // eight chunks asked for before the first is used
-        float part[kAtOnce], l[kAtOnce], a[kAtOnce][kMine];
+        for (int x = 32; x >= 1; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, kWave));
+        const float base = top == neg_inf() ? 0.f : top;
+        constexpr int kMine = DH < kWave ? 1 : DH / kWave, kAtOnce = 8;
+        float o[kMine] = {}, sum = 0.f;
+        for (int c0 = 0; c0 < chunks; c0 += kAtOnce) {          // eight chunks asked for before the first is used
+            float part[kAtOnce], l[kAtOnce], a[kAtOnce][kMine];
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            const int64_t at = first + min(c0 + i, chunks - 1) * apart;
-            part[i] = p.split_ml[2 * at];
-            l[i] = p.split_ml[2 * at + 1];
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int64_t at = first + min(c0 + i, chunks - 1) * apart;
+                part[i] = p.split_ml[2 * at];
+                l[i] = p.split_ml[2 * at + 1];
 #pragma unroll
-            for (int x = 0; x < kMine; ++x) a[i][x] = p.split_acc[at * DH + min(lane + 64 * x, DH - 1)];
-        }
+                for (int x = 0; x < kMine; ++x) a[i][x] = p.split_acc[at * DH + min(lane + 64 * x, DH - 1)];
+            }
 #pragma unroll
-        for (int i = 0; i < kAtOnce; ++i) {
-            if (c0 + i < chunks) {
-                const float weight = __builtin_amdgcn_exp2f(part[i] - base);
-                sum += weight * l[i];
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (c0 + i < chunks) {
+                    const float weight = __builtin_amdgcn_exp2f(part[i] - base);
+                    sum += weight * l[i];
 #pragma unroll
-                for (int x = 0; x < kMine; ++x) o[x] += weight * a[i][x];
+                    for (int x = 0; x < kMine; ++x) o[x] += weight * a[i][x];
+                }
             }
         }
-    }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    if (p.lse && lane == 0) p.lse[(int64_t)head * p.n_q + at_row] = sum == 0.f ? neg_inf() : (top + __log2f(sum)) * kLn2;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (p.lse && lane == 0) p.lse[(int64_t)head * p.n_q + at_row] = sum == 0.f ? neg_inf() : (top + __log2f(sum)) * kLn2;
 #pragma unroll
-    for (int x = 0; x < kMine; ++x) {
-        const int col = lane + 64 * x;
-        if (col >= p.width) continue;
-        const int64_t at = (at_row * p.heads + head) * p.width + col;
-        const float v = o[x] * inv;
-        if constexpr (sizeof(T) == 4) static_cast<T *>(p.out)[at] = v;
-        else static_cast<T *>(p.out)[at].bits = (uint16_t)f32_to_bf16_bits(v);
-        if (p.out_f32) p.out_f32[at] = v;
+        for (int x = 0; x < kMine; ++x) {
+            const int col = lane + 64 * x;
+            if (col >= p.width) continue;
+            const int64_t at = (at_row * p.heads + head) * p.width + col;
+            const float v = o[x] * inv;
+            if constexpr (sizeof(T) == 4) static_cast<T *>(p.out)[at] = v;
+            else static_cast<T *>(p.out)[at].bits = (uint16_t)f32_to_bf16_bits(v);
+            if (p.out_f32) p.out_f32[at] = v;
+        }
     }
 }
 
@@ -708,7 +708,8 @@ int fs_jagged_attention(fs_ctx *ctx, const fs_attention_args *args, fs_stream st
             const int done = launch_attention(ctx, attn_split_kernel<T, DH>, attn_slots(a.n_kv, a.batch, p.split_shift) * a.kv_heads,
                                               lds, s, "attn_split", p);
             if (done != FS_OK || a.n_kv <= 1ll << p.split_shift) return done;     // nobody has several chunks
-            return launch_attention(ctx, attn_join_kernel<T, DH>, ceil_div(a.n_q * a.heads, kAttnWaves), 0, s, "attn_join", p);
+            const int64_t groups = ceil_div(a.n_q * a.heads, kAttnWaves);         // rows are not bounded by attn_check
+            return launch_attention(ctx, attn_join_kernel<T, DH>, groups < kMaxGroups ? groups : kMaxGroups - 1, 0, s, "attn_join", p);
         }
         const auto run = [&](auto exact) {
             const size_t lds = 2 * sizeof(tile<T, DH>) + kAttnWaves * sizeof(uint32_t) +
