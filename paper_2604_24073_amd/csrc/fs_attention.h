@@ -423,14 +423,17 @@ template <typename T, int DH>
 constexpr int attn_waves = sizeof(T) * DH <= 256 ? 2 : 1;
 
 // ---- host side --------------------------------------------------------------------------------------------------------------
-constexpr int kMaxLds = 160 * 1024;
-constexpr int kFreeLds = 64 * 1024;           // what a kernel may ask for without saying so beforehand
+// The compiler's reduction behind __syncthreads_or has 512 bytes of a workgroup's LDS.  Every kernel is allowed all of the rest
+// (the largest asks for 135 KB) and not what one call needs: threads of the host whose tables differ share that allowance.
+constexpr int kStaticLds = 512;
+constexpr int kMaxLds = 160 * 1024 - kStaticLds;
+constexpr int kFreeLds = 64 * 1024 - kStaticLds;           // what a kernel may ask for without saying so beforehand
 
 template <typename F>
 int launch_attention(fs_ctx *ctx, F *kernel, int64_t groups, size_t lds, hipStream_t s, const char *name, const attn_params &p) {
     if (lds > (size_t)kMaxLds) return set_err(ctx, FS_EINVAL, "jagged attention: head_dim, buckets and distances do not fit together");
     if (lds > (size_t)kFreeLds)
-        FS_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+        FS_HIP(ctx, hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds));
     kernel<<<(unsigned)groups, kAttnThreads, lds, s>>>(p);
     FS_LAUNCH_CHECK(ctx, name);
     return FS_OK;
