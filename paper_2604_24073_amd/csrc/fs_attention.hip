@@ -120,6 +120,7 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_para
                     for (int t = 0; t < QT; ++t) mma(s[t][k], a, qf[t][c]);
                 }
             }
+            settle();
             // element r of s[t][k]: query row wrow + 16 t + j, key key0 + 16 k + 4 g + r
             const int nearest = wpos - (key0 + kTile - 1), furthest = wpos + 16 * QT - 1 - key0;
             if (nearest >= bias.high || furthest <= bias.low) {

@@ -322,6 +322,7 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
                         for (int t = 0; t < QT; ++t) mma(dp[t], a, of[t][c]);
                     }
                     f32x4 x;
+                    if constexpr (mask()) settle();                                // what follows may be branches
                     if constexpr (mask()) x = *reinterpret_cast<const f32x4 *>(mark + 16 * k + 4 * g);
 #pragma unroll
                     for (int t = 0; t < QT; ++t) {
@@ -543,6 +544,7 @@ void attn_dkv_kernel(attn_params p) {
                     }
                     f32x4 mq, mo;
                     if constexpr (mask()) {
+                        settle();                                                 // what follows may be branches
                         mq = *reinterpret_cast<const f32x4 *>(mark + at);
                         mo = *reinterpret_cast<const f32x4 *>(mark + kTile + at);
                     }
