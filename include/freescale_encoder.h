@@ -87,7 +87,8 @@ int fs_block_norm(fs_ctx *ctx, const fs_block_args *args, fs_stream stream);
  * Reads y as the forward pass left it (x where a was NULL), a, g, w_post, scale, w_pre; x, h are not read.  Each of y, a, g
  * may be NULL with its codes and exps given instead: the gradient is then taken at the values those stand for.  To leave
  * the join out, a and a_codes are both NULL.  The norms are computed anew from the rows.  dx may be dy.
- * n == 0: the sums over the rows are written, as zeros.
+ * n == 0: those of dw_post, dscale (together) and dw_pre that are not NULL are written, as zeros, and no other entry tells what
+ * is wanted.
  * work: fs_block_norm_work_bytes(n, dim) bytes, contents irrelevant before and after. */
 int fs_block_norm_backward(fs_ctx *ctx, const fs_block_args *args, fs_stream stream);
 size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);

@@ -625,7 +625,7 @@ int attn_check(fs_ctx *ctx, const fs_attention_args &a) {
             "jagged attention: a stride is less than its row or not a multiple of 16 bytes");
     if (a.n_q > 0) FS_NEED(a.q && a.out, "jagged attention: null pointer");
     if (a.n_kv > 0) FS_NEED(a.k && a.v, "jagged attention: null pointer");
-    FS_NEED(aligned16(a.q) && aligned16(a.k) && aligned16(a.v) && aligned16(a.out) && aligned16(a.out_f32),
+    FS_NEED(aligned16(a.q) && aligned16(a.k) && aligned16(a.v) && aligned16(a.out) && (a.dt == FS_F32 || aligned16(a.out_f32)),
             "jagged attention: pointer not 16-byte aligned");
     return FS_OK;
 }

@@ -446,8 +446,8 @@ int fs_block_norm_backward(fs_ctx *ctx, const fs_block_args *args, fs_stream str
             FS_NEED(p.a || p.a_exps, "block norm backward: codes without exponents");
             FS_NEED(p.g || (p.g_codes && p.g_exps), "block norm backward: g is null, or codes without exponents");
             FS_NEED(p.w_post && p.scale && p.da && p.dg, "block norm backward: null pointer");
-            FS_NEED(aligned16(p.w_post) && aligned16(p.scale) && aligned16(p.a) && aligned16(p.g) && aligned16(p.a_codes) &&
-                        aligned16(p.g_codes) && aligned16(p.da) && aligned16(p.dg),
+            FS_NEED(aligned16(p.w_post) && aligned16(p.scale) && aligned16(p.a ? p.a : p.a_codes) && aligned16(p.g ? p.g : p.g_codes) &&
+                        aligned16(p.da) && aligned16(p.dg),
                     "block norm backward: pointer not 16-byte aligned");
             FS_NEED((!p.a || stride_ok(p.a_stride, p.dim, p.dt)) && (!p.g || stride_ok(p.g_stride, p.dim, p.dt)) &&
                         stride_ok(p.da_stride, p.dim, p.dt) && stride_ok(p.dg_stride, p.dim, p.dt),
@@ -456,7 +456,7 @@ int fs_block_norm_backward(fs_ctx *ctx, const fs_block_args *args, fs_stream str
         if (norm) {
             FS_NEED(p.y || (p.y_codes && p.y_exps), "block norm backward: y is null, or codes without exponents");
             FS_NEED(p.w_pre && p.dw_pre, "block norm backward: null pointer");
-            FS_NEED(aligned16(p.y) && aligned16(p.y_codes) && aligned16(p.dh) && aligned16(p.w_pre),
+            FS_NEED(aligned16(p.y ? p.y : p.y_codes) && aligned16(p.dh) && aligned16(p.w_pre),
                     "block norm backward: pointer not 16-byte aligned");
         }
         FS_NEED(p.dx && aligned16(p.dx) && aligned16(p.dy), "block norm backward: dx is null, or dx or dy not 16-byte aligned");
