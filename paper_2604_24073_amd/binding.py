@@ -754,12 +754,14 @@ def _code(what: str, dtype: torch.dtype) -> int:
 def _addr(what: str, t: torch.Tensor, shape, dtype: torch.dtype, device: int) -> int:
     """The address of a contiguous tensor of that shape and type on that GPU; raises if it is not one.  (These checks are most
     of what a small call costs the host: one condition of four quick questions, and the explanation only where one fails.)"""
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+    if t is None or t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
         _refuse(what, t, shape, dtype, device)
     return t.data_ptr()
 
 
 def _refuse(what, t, shape, dtype, device):
+    if t is None:
+        raise ValueError(f"{what}: is needed")
     if t.dtype != dtype:
         raise TypeError(f"{what}: {t.dtype}, {dtype} is needed")
     if tuple(t.shape) != tuple(shape):
@@ -771,7 +773,7 @@ def _refuse(what, t, shape, dtype, device):
 
 def _row_addr(what: str, t: torch.Tensor, shape, dtype: torch.dtype, device: int):
     """(address, elements from row to row) of a tensor whose rows may lie apart; a row itself may not."""
-    if t.is_contiguous():
+    if t is None or t.is_contiguous():
         stride = 1
         for k in shape[1:]:
             stride *= k
@@ -797,6 +799,8 @@ def _alloc_rows8(n: int, dim: int, device) -> Rows8:
 
 
 def _matrix(what: str, t: torch.Tensor):
+    if t is None:
+        raise ValueError(f"{what}: is needed")
     if t.dim() != 2:
         raise ValueError(f"{what}: shape {tuple(t.shape)}, two dimensions are needed")
     return tuple(t.shape)
@@ -955,7 +959,10 @@ def _attention_record(ctx, q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_l
     if kv_lengths is not None:
         rec.kv_lengths = _addr("kv_lengths", kv_lengths, (users[0] - 1,), i64, dev)
     if bias is not None:
-        buckets, size = bias.shape[0], bucket_of.numel()
+        buckets, _ = _matrix("bias", bias)
+        if bucket_of is None or buckets == 0:
+            raise ValueError("bucket_of: is needed" if bucket_of is None else "bias: has no bucket")
+        size = bucket_of.numel()
         if not causal and size % 2 == 0:
             raise ValueError(f"bucket_of: {size} entries, an odd number is needed for distances on both sides")
         rec.bias = _addr("bias", bias, (buckets, heads), torch.float32, dev)
