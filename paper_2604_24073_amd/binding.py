@@ -980,7 +980,7 @@ def fs_jagged_attention(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch
     """out [n_q, heads, head_dim]; keep: also what fs_jagged_attention_backward reads (lse, and out_f32 of bf16 rows).  scale:
     1 / sqrt(head_dim) unless given.  `out`: the caller's tensors under the same names."""
     rec, shape, _ = _attention_record(ctx, q, k, v, q_offsets, kv_offsets, bias, bucket_of, kv_lengths, causal, scale)
-    rec.max_q = max_q
+    rec.max_q = min(max_q, (1 << 31) - 1)                    # 32 bits there; no user has more rows than that
     given, res, dev, f32 = out or {}, {}, ctx.device, torch.float32
     res["out"] = t = given["out"] if "out" in given else torch.empty(shape, dtype=q.dtype, device=q.device)
     rec.out = _addr("out", t, shape, q.dtype, dev)

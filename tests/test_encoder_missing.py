@@ -38,3 +38,13 @@ def test_what_is_missing_is_named(what, call, monkeypatch):
         call(ctx)
     assert str(refusal.value).startswith(what + ":")
     assert not ctx.lib.calls
+
+
+@pytest.mark.parametrize("max_q,want", [(0, 0), (3, 3), (-1, -1), ((1 << 31) - 1, (1 << 31) - 1), (1 << 31, (1 << 31) - 1),
+                                        ((1 << 32) + 1, (1 << 31) - 1), (1 << 70, (1 << 31) - 1)])
+def test_a_bound_of_rows_beyond_32_bits(max_q, want, monkeypatch):
+    monkeypatch.setattr(fs.binding, "_current_raw_stream", lambda device: 1)
+    ctx, seen = Context(), []
+    ctx.lib.fs_jagged_attention = lambda handle, rec, stream: seen.append(rec.max_q) or 0
+    attend(ctx, max_q=max_q)
+    assert seen == [want]
