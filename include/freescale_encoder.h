@@ -35,8 +35,8 @@ extern "C" {
  *     value = code * 2^(exp - 127)
  * The power of two is the smallest for which the largest magnitude of the group rounds to at most 127 steps and is at
  * least 2^-126 (at most 2^121, where magnitudes from 127.5 * 2^121 on become 127 steps: 128 are beyond fp32); codes are
- * rounded to nearest even.  An element is off by at most 1/127 of the group's largest magnitude.  A group with an
- * infinity or a NaN has exponent 255 and reads back as NaN throughout.
+ * rounded to nearest even.  An element is off by at most 1/127 of the group's largest magnitude, or by 2^-127 where that is
+ * more (magnitudes below 127 * 2^-127).  A group with an infinity or a NaN has exponent 255 and reads back as NaN throughout.
  * dim a multiple of FS_ROWS8_GROUP, at most FS_MAX_BLOCK_DIM. */
 int fs_rows_pack8(fs_ctx *ctx, const void *rows, int64_t stride, fs_dtype dt, int64_t n, int32_t dim, int8_t *codes,
                   uint8_t *exps, fs_stream stream);

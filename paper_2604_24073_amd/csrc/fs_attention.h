@@ -419,7 +419,8 @@ constexpr bool from_less = sizeof(T) == 2;
 // Wavefronts of a SIMD that a kernel is compiled for.  With two or more of them asked for, all of a wavefront's registers can be
 // named by every instruction, and the accumulators stay where the vector units can read them.  One / two, backward: rows of 256
 // bytes (64 histories of 2000 up, bf16) keys 2.40 ms / 1.33; of 512 bytes (32 of 2000 up, fp32), which spill then, query rows 2.68 /
-// 4.44.
+// 4.44.  Scalar registers spill in all of them, 65 to 164 of the keys' kernels up to 64 columns and 340 to 370 at 128, and 3 to 5
+// vector registers of the keys' kernels with 256 of them.
 template <typename T, int DH>
 constexpr int attn_waves = sizeof(T) * DH <= 256 ? 2 : 1;
 

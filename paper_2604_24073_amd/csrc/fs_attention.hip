@@ -7,11 +7,11 @@
 // this one is worked on.  The products are turned over: S^T = K Q^T and O^T = V^T P^T, so that a lane has one query
 // row, its m and l are a register each, and the scores stay in registers from one product to the other.
 //
-// Bound by the vector units, which have some ten instructions for a score beside the power's four slots, and by how little of
-// that the matrix units' time hides under (67 % and 36 % of the time, histories of 16384 rows, two wavefronts a SIMD).  160
-// histories with 150 k rows, 8 of them of 16384, 4 heads of 64 columns over 2 key heads, out unrounded for the bias's gradient:
-// 2.7 to 2.9 ms, 400 TFLOP/s of the formula's products and 800 of those that are made.  1024 histories with 262 k rows, 4 heads
-// of 32: 0.50 ms.  Tried without gain: the next tile's scores made beside this tile's powers (registers: a wavefront a SIMD
+// Bound by the vector units, which have 12 to 14 instructions for a score where out is wanted unrounded (five or six of them
+// split P into three terms), and by how little of that the matrix units' time hides under: 73 % and 38 % of the time with 64
+// columns (four wavefronts a SIMD), 84 % and 20 % with 32 (five).  160 histories with 150 k rows, 8 of them of 16384, 4 heads of
+// 64 columns over 2 key heads, out unrounded for the bias's gradient: 2.7 to 2.9 ms, 400 TFLOP/s of the formula's products and
+// 800 of those that are made.  1024 histories with 262 k rows, 4 heads of 32: 0.51 ms.  Tried without gain: the next tile's scores made beside this tile's powers (registers: a wavefront a SIMD
 // less, 0.51 ms to 0.62), priorities for wavefronts in their products.
 #include "fs_attention.h"
 
@@ -28,6 +28,8 @@ constexpr int QT = 1;
 // bias's gradient adds up differences of dO V^T and D = dO . out that cancel over a row, and an out made of rounded P leaves its
 // errors in them.  dbias is off by 6e-4 of itself with one term, 1e-6 with two, 4e-7 with three (1024 histories with 262 k rows,
 // 64 buckets, and histories of 16384 rows alike); the pass over the former, 4 heads of 32 columns, took 0.41, 0.47 and 0.54 ms.
+// Otherwise P is one term: a bf16 out is rounded to half a step of bf16 anyway, and half a step of every P, independent of each
+// other, adds no more than that to it (2.4e-3 off in all against 1.7e-3 for the rounding of out alone).
 template <typename T, int DH, bool EXACT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_params p) {
     constexpr int kRows = 16 * kAttnWaves * QT, kShift = 6, kPad = row_pad(QT);
@@ -432,7 +434,7 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
                 }
 #pragma unroll
             for (int c = 0; c < kSplitKeys / 32; ++c) {
-                piece<T> pf;
+                piece<T> pf;                            // P in one term of T, as in the other form without out_f32
                 as_operand(pf, s[2 * c], s[2 * c + 1]);
 #pragma unroll
                 for (int d = 0; d < MT; ++d) {

@@ -10,7 +10,7 @@
 // loaded it, eight columns each, so that everything is read once and written once, and the norms of the backward pass are
 // computed anew from the rows instead of being kept.  Bound by memory; no product is shared between rows, hence no MFMA.
 // 297 k rows of 128 columns, residual rows fp32 and the block's bf16: forward 532 MB in 102 us, backward 836 MB in 160, both
-// 5.2 TB/s, where a large copy has 4.8; with a and g kept in 8 bits besides (200 k x 256) 822 MB in 148 and 1027 MB in 203.
+// 5.2 TB/s, where a large copy has 6.2; with a and g kept in 8 bits besides (200 k x 256) 822 MB in 148 and 1027 MB in 203.
 // Few rows are launches: 256 x 512 4.6 us forward.
 #include <type_traits>
 
