@@ -116,15 +116,15 @@ __device__ __forceinline__ float row_total(const float *skew, int row) {
     }
     return sum;
 }
-// near: the sum of distance `lane`; far: of distance 64 + lane, where there is one
-__device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], float &near, float &far) {
+// near: the sum of distance `lane`; far: of distance 64 + lane, where there is one.  live: the lane's row exists
+__device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], bool live, float &near, float &far) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
         const int d = j + 63 - 4 * g - r;                  // of key 4 g + r; sixteen keys further on the places turn alike
         float *at = skew + 16 * d + 4 * ((j >> 2) ^ ((d >> 2) & 3)) + (j & 3);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) at[-256 * k] = s[k][r];
+        for (int k = 0; k < 4; ++k) at[-256 * k] = live ? s[k][r] : 0.f;
     }
     wave_lds_order();
     near = row_total(skew, lane);
@@ -132,13 +132,28 @@ __device__ __forceinline__ void diagonal_sums(float *skew, const f32x4 (&s)[4], 
     wave_lds_order();
 }
 
+// a lane's values, those of the first `rows` rows
+template <int QT>
+__device__ __forceinline__ float lane_sum(const f32x4 (&s)[QT][4], int rows) {
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        float row = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) row += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
+        sum += 16 * t + (int)(threadIdx.x & 15) < rows ? row : 0.f;
+    }
+    return sum;
+}
+
 // The 16 QT x 64 values s of a wavefront added to the sums of their buckets; b0: the bucket of the lane's of the first 64
 // distances, b1: of those behind them, the last one's in the lanes that have none.  Tables of distances have few buckets in so
 // many distances but near zero: one bucket takes every lane's sum as it is, two are told apart by comparing distances, and only
 // more are brought into the order of the distances.  Further distances come first: the tiles go from far to near, and a
-// bucket's lanes are added up when the next bucket begins.
+// bucket's lanes are added up when the next bucket begins.  The first `rows` rows exist (any number); the others have whatever the
+// keys made of them, a NaN if one of those is none, and are left out where a lane, which has one row, has its sum.
 template <int QT>
-__device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, const f32x4 (&s)[QT][4], int b0, int b1) {
+__device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, const f32x4 (&s)[QT][4], int rows, int b0, int b1) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
     const int last0 = __builtin_amdgcn_readlane(b0, 63), before0 = __builtin_amdgcn_update_dpp(b0, b0, 0x138, 0xf, 0xf, false);
     int before1 = __builtin_amdgcn_update_dpp(b1, b1, 0x138, 0xf, 0xf, false);
@@ -146,36 +161,35 @@ __device__ __forceinline__ void add_by_bucket(bucket_sums &sums, float *skew, co
     const uint64_t h0 = __ballot(b0 != before0), h1 = __ballot(b1 != before1);    // where a bucket begins
     const int changes = __popcll(h0) + __popcll(h1);
     if (changes == 0) {
-        float all = 0.f;
-#pragma unroll
-        for (int t = 0; t < QT; ++t)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) all += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
-        sums.one(__builtin_amdgcn_readfirstlane(b0), all);
+        sums.one(__builtin_amdgcn_readfirstlane(b0), lane_sum<QT>(s, rows));
     } else if (changes == 1) {
         // the distances from `at` on have another bucket than those before
         const int at = h0 ? 63 - __clzll((long long)h0) : 127 - __clzll((long long)h1);
         const int mine = j + 63 - 4 * g;                   // element r of s[t][k] has distance mine + 16 t - 16 k - r
         float near = 0.f, far = 0.f;
 #pragma unroll
-        for (int t = 0; t < QT; ++t)
+        for (int t = 0; t < QT; ++t) {
+            float near_t = 0.f, far_t = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
                     const bool beyond = mine >= at + 16 * k + r - 16 * t;
-                    far += beyond ? s[t][k][r] : 0.f;
-                    near += beyond ? 0.f : s[t][k][r];
+                    far_t += beyond ? s[t][k][r] : 0.f;
+                    near_t += beyond ? 0.f : s[t][k][r];
                 }
+            far += 16 * t + j < rows ? far_t : 0.f;
+            near += 16 * t + j < rows ? near_t : 0.f;
+        }
         sums.one(__builtin_amdgcn_readlane(b1, 63), far);    // the last distance's
         sums.one(__builtin_amdgcn_readfirstlane(b0), near);
     } else {
         float near, far;
-        diagonal_sums(skew, s[0], near, far);
+        diagonal_sums(skew, s[0], j < rows, near, far);
         if constexpr (QT == 2) {
             // the second sixteen rows' distances are sixteen further on
             float near2, far2;
-            diagonal_sums(skew, s[1], near2, far2);
+            diagonal_sums(skew, s[1], 16 + j < rows, near2, far2);
             const float y = __shfl(near2, (lane + 48) & 63, kWave), z = __shfl(far2, (lane + 48) & 63, kWave);
             near += lane >= 16 ? y : 0.f;
             far += lane < 16 ? y : z;                      // z: zeros from distance 95 on
@@ -364,14 +378,9 @@ __global__ __launch_bounds__(kAttnThreads, (attn_waves<T, DH>)) void attn_dq_ker
             else work(std::false_type(), std::false_type());
             if (part) {
                 if (all_far) {
-                    float share = 0.f;
-#pragma unroll
-                    for (int t = 0; t < QT; ++t)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) share += (s[t][k][0] + s[t][k][1]) + (s[t][k][2] + s[t][k][3]);
-                    sums.one(__builtin_amdgcn_readfirstlane(bias.bucket(p, buckets[0])), share);
+                    sums.one(__builtin_amdgcn_readfirstlane(bias.bucket(p, buckets[0])), lane_sum<QT>(s, u.nq - wrow));
                 } else {
-                    add_by_bucket<QT>(sums, skew + w * kSkew, s, bias.bucket(p, buckets[0]), bias.bucket(p, buckets[1]));
+                    add_by_bucket<QT>(sums, skew + w * kSkew, s, u.nq - wrow, bias.bucket(p, buckets[0]), bias.bucket(p, buckets[1]));
                 }
             }
         }
