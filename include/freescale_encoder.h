@@ -122,17 +122,17 @@ size_t fs_block_norm_work_bytes(int64_t n, int32_t dim);
  *   lse   [heads, n_q] fp32 (OPTIONAL; the backward pass reads it): log of the sum of exp(s_i), -infinity for a row that sees
  *         nothing
  *   out_f32 [n_q, heads, head_dim] fp32 (OPTIONAL, bf16 only): out before its rounding.  The backward pass reads it where it
- *         is given: without it, dbias carries the roundings of out (and of P, behind the form for single tokens).
+ *         is given: without it, dbias carries the roundings of out.
  *   max_q no user has more query rows than this (0: unknown).  With max_q * heads / kv_heads <= 16 the keys are cut up over
  *         the chip, which is the form for single tokens; a user with more rows is then reported as FS_ERANGE and its rows of
  *         out are left as they were.
  *   work  fs_jagged_attention_work_bytes(args) bytes, 16-byte aligned, contents irrelevant (0 bytes and NULL but for the form
  *         above)
- * scale is positive.  Scores, softmax and sums are in fp32; P and dS are rounded to dt where they go into a product.  head_dim
- * a multiple of 4 (fp32) / 8 (bf16), at most FS_MAX_HEAD_DIM; strides of q, k and v at most FS_MAX_ROW_STRIDE.
- * (rows / 64 + batch) * heads < 2^24, and a user has fewer than 2^30 rows.  Boundaries that do not ascend from 0 to n_q (n_kv)
- * and lengths that do not fit their room are reported as FS_ERANGE by fs_check_async; out of the user concerned is not written
- * or is that of the keys there are. */
+ * scale is positive.  Scores, softmax and sums are in fp32; P and dS are rounded to dt where they go into a product, but for P of
+ * out_f32 and of the form for single tokens, which keeps its 24 bits.  head_dim a multiple of 4 (fp32) / 8 (bf16), at most
+ * FS_MAX_HEAD_DIM; strides of q, k and v at most FS_MAX_ROW_STRIDE.  (rows / 64 + batch) * heads < 2^24, and a user has fewer
+ * than 2^30 rows.  Boundaries that do not ascend from 0 to n_q (n_kv) and lengths that do not fit their room are reported as
+ * FS_ERANGE by fs_check_async; out of the user concerned is not written or is that of the keys there are. */
 typedef struct fs_attention_args {
     const void *q, *k, *v;
     int64_t q_stride, k_stride, v_stride;
@@ -163,6 +163,8 @@ size_t fs_jagged_attention_work_bytes(const fs_attention_args *args);
  *     dq, dk, dv of dt, rows dq_stride, dk_stride, dv_stride elements apart; rows of k and v that are not in use get zeros
  *     dbias [num_buckets, heads] fp32 (NULL: not wanted), overwritten; what fs_rowwise_adagrad_update takes as `reduced` with
  *     the bias as a table of num_buckets rows of `heads` columns
+ * Where a pair that is seen has an infinity or a NaN in it, the gradients that it goes into may be NaN where the formula has a
+ * number.
  * work: fs_jagged_attention_backward_work_bytes(args) bytes, 16-byte aligned, contents irrelevant. */
 int fs_jagged_attention_backward(fs_ctx *ctx, const fs_attention_args *args, fs_stream stream);
 size_t fs_jagged_attention_backward_work_bytes(const fs_attention_args *args);

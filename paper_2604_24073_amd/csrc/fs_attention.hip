@@ -28,7 +28,7 @@ constexpr int QT = 1;
 // bias's gradient adds up differences of dO V^T and D = dO . out that cancel over a row, and an out made of rounded P leaves its
 // errors in them.  dbias is off by 6e-4 of itself with one term, 1e-6 with two, 4e-7 with three (1024 histories with 262 k rows,
 // 64 buckets, and histories of 16384 rows alike); the pass over the former, 4 heads of 32 columns, took 0.41, 0.47 and 0.54 ms.
-// Otherwise P is one term: a bf16 out is rounded to half a step of bf16 anyway, and half a step of every P, independent of each
+// Without out_f32 P is one term: a bf16 out is rounded to half a step of bf16 anyway, and half a step of every P, independent of each
 // other, adds no more than that to it (2.4e-3 off in all against 1.7e-3 for the rounding of out alone).
 template <typename T, int DH, bool EXACT>
 __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_params p) {
@@ -297,7 +297,8 @@ __global__ __launch_bounds__(kAttnThreads, 2) void attn_forward_kernel(attn_para
 // cut up: a workgroup has a chunk of one user's keys for all query rows and heads that share a key head (at most sixteen
 // columns of a product), its wavefronts take kSplitKeys keys each in turn, and what they have of m, l and o is put together, in
 // the workgroup first, then, where a user has several chunks, by a second launch.  Bound by the waits of one chunk, one behind
-// the other, more than by memory: 256 users with 93 k keys, 8 heads of 64 columns over 2, 47 MB: 20 us (2.4 TB/s) and 7.
+// the other, more than by memory: 256 users with 93 k keys, 8 heads of 64 columns over 2, 47 MB: 20.6 us (2.3 TB/s) and 6.  Here
+// P is three terms of bf16 always, as the matrix units have the time for it (19.5 us with one term).
 constexpr int kSplitCols = 16;
 constexpr int kSplitKeys = 32;                        // keys of a wavefront at a time
 constexpr int kSplitStep = kAttnWaves * kSplitKeys;   // keys of a workgroup at a time
@@ -346,7 +347,9 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
     const float scale2 = p.scale * kLog2e;
     const int high = p.distances - 1, low = p.causal ? 0 : -high;
 
-    f32x4 acc[MT] = {};
+    // further terms of P in bf16, with a sum of their own as in attn_forward_kernel
+    constexpr int kMore = sizeof(T) == 2 ? 2 : 0;
+    f32x4 acc[MT] = {}, acc_rest[kMore ? MT : 1] = {};
     float m = neg_inf(), l = 0.f;
     const int met = kSplitStep + u.nq - 1;                // distances of a step's keys from the query rows
     for (int step = begin; step < stop; step += kSplitStep) {
@@ -424,7 +427,10 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
 #pragma unroll
             for (int d = 0; d < MT; ++d)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[d][r] *= shrink;
+                for (int r = 0; r < 4; ++r) {
+                    acc[d][r] *= shrink;
+                    if constexpr (kMore > 0) acc_rest[d][r] *= shrink;
+                }
 #pragma unroll
             for (int k = 0; k < kSplitKeys / 16; ++k)
 #pragma unroll
@@ -434,13 +440,21 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
                 }
 #pragma unroll
             for (int c = 0; c < kSplitKeys / 32; ++c) {
-                piece<T> pf;                            // P in one term of T, as in the other form without out_f32
-                as_operand(pf, s[2 * c], s[2 * c + 1]);
+                piece<T> pf, rest[kMore ? kMore : 1];
+                if constexpr (kMore > 0) {
+                    take_operand(pf, s[2 * c], s[2 * c + 1]);
+#pragma unroll
+                    for (int i = 0; i < kMore; ++i) take_operand(rest[i], s[2 * c], s[2 * c + 1]);
+                } else {
+                    as_operand(pf, s[2 * c], s[2 * c + 1]);
+                }
 #pragma unroll
                 for (int d = 0; d < MT; ++d) {
                     piece<T> a;
                     vt[w].cols(a, 32 * c, 16 * d);
                     mma(acc[d], a, pf);
+#pragma unroll
+                    for (int i = 0; i < kMore; ++i) mma(acc_rest[d], a, rest[i]);
                 }
             }
             settle();
@@ -469,7 +483,13 @@ __global__ __launch_bounds__(kAttnThreads, (split_waves<T, DH>)) void attn_split
         ml[2 * (w * kSplitCols + j) + 1] = l;
     }
 #pragma unroll
-    for (int d = 0; d < MT; ++d) *reinterpret_cast<f32x4 *>(os + (w * kSplitCols + j) * kLd + 16 * d + 4 * g) = acc[d];
+    for (int d = 0; d < MT; ++d) {
+        if constexpr (kMore > 0) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[d][r] += fabsf(acc[d][r]) < __builtin_inff() ? acc_rest[d][r] : 0.f;
+        }
+        *reinterpret_cast<f32x4 *>(os + (w * kSplitCols + j) * kLd + 16 * d + 4 * g) = acc[d];
+    }
     __syncthreads();
     const bool whole = u.nk <= chunk;
     for (int x = threadIdx.x; x < cols * (DH / 4); x += kAttnThreads) {

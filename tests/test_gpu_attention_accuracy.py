@@ -97,3 +97,25 @@ def test_the_bounds_tell(causal, width):
     assert all(off(b[:, h], dbias[:, h]) > 5 * DBIAS for h in range(2))
     _, b = plain(c, lost=100)
     assert all(off(b[:, h], dbias[:, h]) > 5 * DBIAS for h in range(2))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("width", [32, 64, 128])
+def test_few_rows_against_caches(dtype, causal, width):
+    """The form for few rows keeps P's bits too, and so does a backward pass behind it."""
+    ctx = fs.Context(max_ids=1024)
+    lens_q, lens_k = [4] * 8, [60, 300, 700, 1500, 90, 257, 256, 33]
+    c = Case(lens_q, lens_k, [n + 5 for n in lens_k], heads=2, kv_heads=1, width=width, dtype=dtype, causal=causal, buckets=6,
+             distances=300, seed=9)
+    c.bucket_of = case(dtype, width, causal).bucket_of
+    want = c.want()
+    kept = c.forward(ctx, keep=True, max_q=4)
+    unrounded = kept["out_f32"] if dtype == BF16 else kept["out"]
+    assert off(unrounded, want["out"][0]) <= OUT and off(kept["lse"], want["lse"][0]) <= OUT
+    dbias, ref = c.backward(ctx, kept)["dbias"], want["dbias"][0]
+    for head in range(2):
+        assert off(dbias[:, head], ref[:, head]) <= DBIAS, head
+    assert fs.fs_check_async(ctx) == fs.FS_OK
+    ctx.close()
