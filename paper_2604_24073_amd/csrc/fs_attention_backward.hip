@@ -12,7 +12,7 @@
 // 160 histories with 150 k rows, 8 of them of 16384, 4 heads of 64 columns over 2 key heads: query rows 2.5 to 2.6 ms (660
 // TFLOP/s of their three products), keys 3.4 to 3.6 (630 of their four).  1024 histories with 262 k rows, 4 heads of 32: 0.67 to
 // 0.72 and 0.58 to 0.61 ms, a third of the former the bias's sums, which tell the buckets of a tile apart.  Of the time the
-// vector units are busy 56 % (query rows, 64 columns; 8.6 instructions a score) and 70 % (32 columns; 18), and no unit of the keys'
+// vector units are busy 56 % (query rows, 64 columns; 8.9 instructions a score) and 71 % (32 columns; 18.5), and no unit of the keys'
 // kernel is busy for long: vector 40 % (7.7 instructions a score), matrix 30 %, LDS 41 % with 64 columns, 60, 17 and 61 % with 32;
 // its wavefronts wait 45 % of their time, and every turn fetches spilled scalars back.  Tiles that are partly seen, all there are
 // in short histories, cost several times the others: their masks are branches for each score.  A second pair of tiles in LDS, to save a barrier a tile, was slower: fewer workgroups fit (0.81 and 0.60).

@@ -113,3 +113,19 @@ def test_in_a_capture_that_forks(ctx):
             for name, t in ref.items():
                 assert torch.equal(res[name], t), name
         calls[1](None)
+
+
+@pytest.mark.parametrize("named", ["handle", "stream"])
+def test_the_default_stream_named_beside_another(ctx, named):
+    """Stream 0 by its handle and by torch's object, while another stream is the current one, which stays that."""
+    calls = [calls_of(ctx, "backward", seed) for seed in (6, 7)]
+    want = [{k: t.clone() for k, t in call(None).items()} for call in calls]
+    torch.cuda.synchronize()
+    side, default = torch.cuda.Stream(), torch.cuda.default_stream()
+    with torch.cuda.stream(side):
+        got = [calls[0](0 if named == "handle" else default), calls[1](None)]
+        assert torch.cuda.current_stream() == side
+    torch.cuda.synchronize()
+    for res, ref in zip(got, want):
+        for name, t in ref.items():
+            assert torch.equal(res[name], t), name
