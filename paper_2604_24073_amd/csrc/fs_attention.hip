@@ -11,8 +11,9 @@
 // split P into three terms), and by how little of that the matrix units' time hides under: 73 % and 38 % of the time with 64
 // columns (four wavefronts a SIMD), 84 % and 20 % with 32 (five).  160 histories with 150 k rows, 8 of them of 16384, 4 heads of
 // 64 columns over 2 key heads, out unrounded for the bias's gradient: 2.7 to 2.9 ms, 400 TFLOP/s of the formula's products and
-// 800 of those that are made.  1024 histories with 262 k rows, 4 heads of 32: 0.51 ms.  Tried without gain: the next tile's scores made beside this tile's powers (registers: a wavefront a SIMD
-// less, 0.51 ms to 0.62), priorities for wavefronts in their products.
+// 800 of those that are made.  1024 histories with 262 k rows, 4 heads of 32: 0.51 ms.  Tried without gain: the next tile's
+// scores made beside this tile's powers (registers: a wavefront a SIMD less, 0.51 ms to 0.62), priorities for wavefronts in their
+// products.
 #include "fs_attention.h"
 
 using namespace fs;

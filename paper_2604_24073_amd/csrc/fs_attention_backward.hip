@@ -15,7 +15,8 @@
 // vector units are busy 56 % (query rows, 64 columns; 8.9 instructions a score) and 71 % (32 columns; 18.5), and no unit of the keys'
 // kernel is busy for long: vector 40 % (7.7 instructions a score), matrix 30 %, LDS 41 % with 64 columns, 60, 17 and 61 % with 32;
 // its wavefronts wait 45 % of their time, and every turn fetches spilled scalars back.  Tiles that are partly seen, all there are
-// in short histories, cost several times the others: their masks are branches for each score.  A second pair of tiles in LDS, to save a barrier a tile, was slower: fewer workgroups fit (0.81 and 0.60).
+// in short histories, cost several times the others: their masks are branches for each score.  A second pair of tiles in LDS, to
+// save a barrier a tile, was slower: fewer workgroups fit (0.81 and 0.60).
 #include "fs_attention.h"
 
 using namespace fs;
